@@ -306,6 +306,75 @@ int idkm_code_bits(int k);                   /* 1, 2, 4 or 8; 0 for k outside [1
 size_t idkm_codes_bytes(int64_t m, int k);   /* ceil(m * idkm_code_bits(k) / 8); 0 for bad arguments */
 
 /*
+ * Hard assignment with a scale per group of weights: 4-bit codes for layers whose rows or channels differ too much in size for
+ * one codebook (the paper clusters a layer around one codebook; this is idkm_assign on weights taken relative to their group).
+ * W (DEVICE, [rows][cols], rows ldw elements apart) is of element type w_type, C (DEVICE, k <= 16 entries), scales_out and the
+ * arithmetic below are of element type `type` (0 fp32, 1 bfloat16, 2 IEEE half).  A group is `group` consecutive weights of a
+ * row -- 32, 64 or a multiple of 128; the last of a row may be shorter; group >= cols: one scale per row -- and gets
+ *   s = max|w| / max_j|c_j|, divided in fp32 and rounded to `type`,       scales_out [rows][ceil(cols / group)];
+ * a weight gets the lowest index j among those with the smallest |w - s c_j| (as fp64 arithmetic finds it): 4 bits, the even
+ * column in the low half of a byte, rows of codes_out idkm_group_codes_pitch(cols) = 16 ceil(cols / 32) bytes apart, codes past
+ * the last column 0 -- for a multiple of 32 columns the bytes of idkm_assign with 5 <= k <= 16.  Wq_out (DEVICE,
+ * [rows][cols], contiguous, or NULL) receives s c_j, multiplied in fp32 and rounded to w_type.  Codebook entries that are not
+ * finite are never the nearest and have no part in max_j|c_j|.  A group with a NaN or an infinity, or whose scale leaves the
+ * range of `type`, gets a scale that is not finite and codes 0; where s is 0 (weights all 0, or too small for `type`) the codes
+ * are 0 as well.  codes_out 16-byte aligned; the others to their elements.  No context, no workspace; asynchronous on
+ * cuda_stream; outputs may not overlap inputs.  Returns IDKM_OK, IDKM_ERR_NULL, IDKM_ERR_UNSUPPORTED (k, types, group),
+ * IDKM_ERR_SHAPE, IDKM_ERR_PARAM, IDKM_ERR_ALIGN or IDKM_ERR_CUDA.
+ */
+int idkm_assign_groups(const void* W, int w_type, int64_t rows, int64_t cols, int64_t ldw, const void* C, int k, int type,
+                       int64_t group, unsigned char* codes_out, void* scales_out, void* Wq_out, void* cuda_stream);
+int64_t idkm_group_codes_pitch(int64_t cols);   /* 16 ceil(cols / 32); 0 for cols < 1 */
+
+/*
+ * Products with such weights, without dequantising them in memory:
+ *   Y[m][n] = sum_k s[n][k / group] C[code[n][k]] X[m][k]         (m < tokens, n < rows, k < cols)
+ * for one token or many.  X (rows ldx elements apart), C, scales and Y (rows ldy elements apart) are of element type `type`,
+ * all DEVICE; codes as idkm_assign_groups writes them, rows `pitch` bytes apart (a multiple of 16, at least 16 ceil(cols / 32);
+ * the bytes of a row up to there are read, codes past the last column count for nothing).  scales = NULL: all 1 (the codes of
+ * idkm_assign for a layer of 5 <= k <= 16 scalar centroids and rows of a multiple of 32 weights).  Products and sums are in
+ * fp32, the scale multiplies the fp32 sum of its group, and Y is rounded once; the order of the sums depends on the shape
+ * alone.  C must be finite; a code that names no entry stands for 0.  codes 16-byte aligned, the others to their elements
+ * (X is read fastest from 16-byte-aligned rows).  Y may not overlap an input.  No context, no workspace; asynchronous on
+ * cuda_stream.  Returns as idkm_assign_groups.
+ */
+int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_t ldx, const unsigned char* codes, int64_t rows, int64_t cols,
+                      int64_t pitch, const void* C, int k, const void* scales, int64_t group, void* Y, int64_t ldy,
+                      void* cuda_stream);
+
+/*
+ * Distillation from a teacher's top logits: the loss by which a quantised network (Algorithm 2: "L(network(Wq))") is trained
+ * from the full-precision one, and its gradient with respect to the student's logits, from which dL/dWq and then
+ * idkm_backward follow.  (The paper trains on labels; the loss is that of Hinton et al., "Distilling the Knowledge in a Neural
+ * Network", over the entries that were kept.)  For a row z (DEVICE, [rows][vocab], rows ldz elements apart, element type
+ * `type`) and the teacher's entries idx, t (DEVICE, [rows][top], contiguous; indices of idx_bytes = 4 or 8 bytes, logits of
+ * element type t_type; 1 <= top <= IDKM_DISTILL_MAX_TOP):
+ *   p_j = softmax_j(t_j / tau) over the entries with 0 <= idx_j < vocab (others do not count: pad with -1),
+ *   q_v = softmax_v(z_v / tau),
+ *   loss_out[row] = tau^2 sum_j p_j (ln p_j - ln q_{idx_j})                (terms with p_j = 0 are 0),
+ *   dz_out[row][v] = weight[row] tau (q_v - sum_{j: idx_j = v} p_j).
+ * An index given twice counts twice.  A row without entries that count, or whose logits t are all -inf, has loss and gradient
+ * 0.  Logits z of -inf (masked classes) have q = 0; where the teacher has p > 0 for one the loss is +inf.  A row z without a
+ * finite logit has NaN.  weight (DEVICE, fp32 [rows], NULL: 1) is dL/dloss of the row.  fp32 arithmetic.
+ *   idkm_distill_forward   writes the loss (fp32 [rows]) and, for the backward, stats_out (fp32 [rows][2], or NULL): the
+ *                          logarithms of the student's and of the teacher's normaliser, in units of logits / tau;
+ *   idkm_distill_backward  writes dz (rows lddz elements apart, type of z) from the same inputs and those statistics;
+ *   idkm_distill_step      both in one launch, z read once where a row fits on the chip.
+ * dz_out may be z itself (with lddz = ldz), otherwise it may not overlap an input.  No context, no workspace; asynchronous on
+ * cuda_stream.  Returns IDKM_OK, IDKM_ERR_NULL, IDKM_ERR_UNSUPPORTED (types, top), IDKM_ERR_SHAPE, IDKM_ERR_PARAM (tau),
+ * IDKM_ERR_ALIGN (a pointer not aligned to its elements) or IDKM_ERR_CUDA.
+ */
+#define IDKM_DISTILL_MAX_TOP 256
+int idkm_distill_forward(const void* z, int type, int64_t rows, int64_t vocab, int64_t ldz, const void* idx, int idx_bytes,
+                         const void* t, int t_type, int top, float tau, float* loss_out, float* stats_out, void* cuda_stream);
+int idkm_distill_backward(const void* z, int type, int64_t rows, int64_t vocab, int64_t ldz, const void* idx, int idx_bytes,
+                          const void* t, int t_type, int top, float tau, const float* stats, const float* weight, void* dz_out,
+                          int64_t lddz, void* cuda_stream);
+int idkm_distill_step(const void* z, int type, int64_t rows, int64_t vocab, int64_t ldz, const void* idx, int idx_bytes,
+                      const void* t, int t_type, int top, float tau, const float* weight, float* loss_out, void* dz_out,
+                      int64_t lddz, void* cuda_stream);
+
+/*
  * Measured issue rates of the two pipes that bound the arithmetic-bound passes, for roofline denominators (the
  * paper has no counterpart: this is a measurement utility, nothing on the IDKM path calls it).  Two register-only
  * kernels over all SMs -- eight independent chains per thread of fp32 fused multiply-adds, and of ex2.approx --

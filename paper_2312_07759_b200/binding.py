@@ -100,6 +100,20 @@ lib.idkm_code_bits.argtypes = [C.c_int]
 lib.idkm_code_bits.restype = C.c_int
 lib.idkm_codes_bytes.argtypes = [C.c_int64, C.c_int]
 lib.idkm_codes_bytes.restype = C.c_size_t
+lib.idkm_group_codes_pitch.argtypes = [C.c_int64]
+lib.idkm_group_codes_pitch.restype = C.c_int64
+lib.idkm_assign_groups.argtypes = [_vp, C.c_int, C.c_int64, C.c_int64, C.c_int64, _vp, C.c_int, C.c_int, C.c_int64, _vp, _vp, _vp, _vp]
+lib.idkm_assign_groups.restype = C.c_int
+lib.idkm_matmul_codes.argtypes = [_vp, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int64, C.c_int64, C.c_int64, _vp, C.c_int, _vp, C.c_int64,
+                                  _vp, C.c_int64, _vp]
+lib.idkm_matmul_codes.restype = C.c_int
+_logits = [_vp, C.c_int, C.c_int64, C.c_int64, C.c_int64, _vp, C.c_int, _vp, C.c_int, C.c_int, C.c_float]
+lib.idkm_distill_forward.argtypes = _logits + [_vp, _vp, _vp]
+lib.idkm_distill_forward.restype = C.c_int
+lib.idkm_distill_backward.argtypes = _logits + [_vp, _vp, _vp, C.c_int64, _vp]
+lib.idkm_distill_backward.restype = C.c_int
+lib.idkm_distill_step.argtypes = _logits + [_vp, _vp, _vp, C.c_int64, _vp]
+lib.idkm_distill_step.restype = C.c_int
 lib.idkm_status_string.argtypes = [C.c_int]
 lib.idkm_status_string.restype = C.c_char_p
 
@@ -172,6 +186,197 @@ def assign(W, Cm, want_codes: bool = True, want_Wq: bool = True, stream=None):
     _check(lib.idkm_assign(_ptr(W), m, d, _ptr(Cm), k, _ptr(codes) if codes is not None else None,
                            _ptr(Wq) if Wq is not None else None, _stream(stream)))
     return codes, Wq
+
+
+_ELEM = {}   # element types by torch's names for them, as idkm_set_wq_dtype numbers them
+
+
+def _elem(t, *others) -> int:
+    """The number of a tensor's element type; ``others`` have to be of the same."""
+    if not _ELEM:
+        import torch
+        _ELEM.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    e = _ELEM.get(t.dtype)
+    if e is None:
+        raise IdkmError(ERR_UNSUPPORTED)
+    for o in others:
+        if o is not None and o.dtype != t.dtype:
+            raise ValueError(f"tensors of one element type expected: {t.dtype} and {o.dtype}")
+    return e
+
+
+def _ld(t) -> int:
+    """Elements between the rows of a matrix whose rows are contiguous."""
+    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+        raise ValueError(f"a matrix with contiguous rows expected, not shape {tuple(t.shape)} with strides {t.stride()}")
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+class _Place:
+    """Where a call runs: the device of its first tensor, which all of them have to be on, and the stream -- ``stream``, or that
+    device's current one.  Inside the ``with``, new tensors belong to that stream."""
+    __slots__ = ("handle", "_with", "_dev")
+
+    def __init__(self, stream, first, *others):
+        if not first.is_cuda:
+            raise ValueError("tensors on a CUDA device expected")
+        self._dev = dev = first.device
+        for o in others:
+            if o is not None and o.device != dev:
+                raise ValueError(f"tensors on one device expected: {dev} and {o.device}")
+        import torch
+        self._with = None
+        if stream is not None:
+            if not hasattr(stream, "cuda_stream"):
+                stream = torch.cuda.ExternalStream(int(stream), device=dev)
+            if stream.device != dev:
+                raise ValueError(f"a stream of {dev} expected, not of {stream.device}")
+            self._with = torch.cuda.stream(stream)
+            self.handle = int(stream.cuda_stream) or None
+        else:
+            if torch.cuda.current_device() != dev.index:
+                self._with = torch.cuda.device(dev)
+            self.handle = torch._C._cuda_getCurrentRawStream(dev.index) or None
+
+    def __enter__(self):
+        if self._with is not None:
+            self._with.__enter__()
+        return self
+
+    def __exit__(self, *a):
+        if self._with is not None:
+            self._with.__exit__(*a)
+
+
+def _apart(out, *inputs) -> None:
+    """A given output may not share memory with an input."""
+    lo = out.data_ptr()
+    hi = lo + (sum((n - 1) * st for n, st in zip(out.shape, out.stride())) + 1) * out.element_size()
+    for t in inputs:
+        if t is not None and t.numel():
+            a = t.data_ptr()
+            b = a + (sum((n - 1) * st for n, st in zip(t.shape, t.stride())) + 1) * t.element_size()
+            if a < hi and lo < b:
+                raise ValueError("the output shares memory with an input")
+
+
+def assign_groups(W, Cm, group: int, want_Wq: bool = False, stream=None):
+    """``idkm_assign_groups``: 4-bit codes (uint8 [rows, 16 ceil(cols / 32)]), scales ([rows, ceil(cols / group)], of the type of
+    the codebook ``Cm``) and, if wanted, the dequantised weights (of W's type) of a CUDA matrix W; ``Cm`` holds k <= 16 entries."""
+    import torch
+    e, ew, ld = _elem(Cm), _elem(W), _ld(W)
+    rows, cols = W.shape
+    if not Cm.is_contiguous() or group < 1:
+        raise ValueError("a contiguous codebook and a positive group expected")
+    with _Place(stream, W, Cm) as at:
+        dev = W.device
+        codes = torch.empty((rows, (cols + 31) // 32 * 16), dtype=torch.uint8, device=dev)
+        scales = torch.empty((rows, -(-cols // group)), dtype=Cm.dtype, device=dev)
+        Wq = torch.empty((rows, cols), dtype=W.dtype, device=dev) if want_Wq else None
+        rc = lib.idkm_assign_groups(W.data_ptr(), ew, rows, cols, ld, Cm.data_ptr(), Cm.numel(), e, group, codes.data_ptr(),
+                                    scales.data_ptr(), _ptr(Wq), at.handle)
+    _check(rc)
+    return codes, scales, Wq
+
+
+def matmul_codes(X, codes, Cm, scales=None, group: int = 0, out=None, stream=None):
+    """``idkm_matmul_codes``: X [tokens, cols] times the transpose of the weights that ``codes`` ([rows, bytes], uint8, as
+    ``assign_groups`` gives them; those of ``assign`` reshaped to rows) stand for with the codebook ``Cm`` and ``scales``
+    ([rows, ceil(cols / group)], or None); returns [tokens, rows] of X's type, which is that of the codebook and the scales."""
+    import torch
+    e, ldx = _elem(X, Cm, scales), _ld(X)
+    tokens, cols = X.shape
+    pitch, rows = _ld(codes), codes.shape[0]
+    if codes.dtype != torch.uint8 or 2 * codes.shape[1] < cols or not Cm.is_contiguous():
+        raise ValueError("uint8 codes of at least cols / 2 bytes a row and a contiguous codebook expected")
+    if scales is not None and (group < 1 or scales.shape != (rows, -(-cols // group)) or not scales.is_contiguous()):
+        raise ValueError(f"contiguous scales of shape ({rows}, cols / group) expected")
+    if codes.shape[1] < (cols + 31) // 32 * 16:
+        raise IdkmError(ERR_SHAPE)
+    with _Place(stream, X, codes, Cm, scales) as at:
+        if out is None:
+            out = torch.empty((tokens, rows), dtype=X.dtype, device=X.device)
+            ldy = rows
+        else:
+            if out.shape != (tokens, rows) or out.dtype != X.dtype or out.device != X.device:
+                raise ValueError(f"an output of shape ({tokens}, {rows}) and of X's type and device expected")
+            _apart(out, X, codes, Cm, scales)
+            ldy = _ld(out)
+        rc = lib.idkm_matmul_codes(X.data_ptr(), e, tokens, ldx, codes.data_ptr(), rows, cols, pitch, Cm.data_ptr(), Cm.numel(),
+                                   None if scales is None else scales.data_ptr(), group, out.data_ptr(), ldy, at.handle)
+    _check(rc)
+    return out
+
+
+def _distill_inputs(z, idx, t, tau):
+    import torch
+    if idx.dtype not in (torch.int64, torch.int32):
+        raise ValueError("indices of 32 or 64 bits expected")
+    if idx.dim() != 2 or idx.shape != t.shape or idx.shape[0] != z.shape[0] or not idx.is_contiguous() or not t.is_contiguous():
+        raise ValueError("contiguous indices and logits of the teacher of one shape (rows, top) expected")
+    return (z.data_ptr(), _elem(z), z.shape[0], z.shape[1], _ld(z), idx.data_ptr(), 8 if idx.dtype == torch.int64 else 4,
+            t.data_ptr(), _elem(t), idx.shape[1], float(tau))
+
+
+def _row_floats(x, rows, name):
+    import torch
+    if x is not None and (x.dtype != torch.float32 or x.shape != (rows,) or not x.is_contiguous()):
+        raise ValueError(f"{name}: contiguous float32 of shape ({rows},) expected")
+
+
+def _distill_out(z, out, *inputs):
+    import torch
+    if out is None:
+        return torch.empty(z.shape, dtype=z.dtype, device=z.device)
+    if out.shape != z.shape or out.dtype != z.dtype or out.device != z.device:
+        raise ValueError("an output of z's shape, type and device expected")
+    _apart(out, *inputs)
+    if out.data_ptr() != z.data_ptr() or _ld(out) != _ld(z):
+        _apart(out, z)
+    return out
+
+
+def distill_forward(z, idx, t, tau: float, stream=None):
+    """``idkm_distill_forward``: (loss [rows], statistics [rows, 2] for ``distill_backward``), both float32, of the student's logits
+    z [rows, vocab] against the teacher's logits t [rows, top] at the indices idx [rows, top] (int32 or int64; -1: no entry)."""
+    import torch
+    a = _distill_inputs(z, idx, t, tau)
+    with _Place(stream, z, idx, t) as at:
+        loss = torch.empty(z.shape[0], dtype=torch.float32, device=z.device)
+        stats = torch.empty((z.shape[0], 2), dtype=torch.float32, device=z.device)
+        rc = lib.idkm_distill_forward(*a, loss.data_ptr(), stats.data_ptr(), at.handle)
+    _check(rc)
+    return loss, stats
+
+
+def distill_backward(z, idx, t, tau: float, stats, weight=None, out=None, stream=None):
+    """``idkm_distill_backward``: the gradient with respect to z ([rows, vocab], of z's type), rows weighted by ``weight`` (float32
+    [rows], dL/dloss; None: 1), from the statistics of ``distill_forward``.  ``out`` may be z itself."""
+    import torch
+    a = _distill_inputs(z, idx, t, tau)
+    _row_floats(weight, z.shape[0], "weight")
+    if stats.dtype != torch.float32 or stats.shape != (z.shape[0], 2) or not stats.is_contiguous():
+        raise ValueError("the statistics of distill_forward expected")
+    with _Place(stream, z, idx, t, stats, weight) as at:
+        dz = _distill_out(z, out, idx, t, stats, weight)
+        rc = lib.idkm_distill_backward(*a, stats.data_ptr(), None if weight is None else weight.data_ptr(), dz.data_ptr(), _ld(dz),
+                                       at.handle)
+    _check(rc)
+    return dz
+
+
+def distill_step(z, idx, t, tau: float, weight=None, out=None, stream=None):
+    """``idkm_distill_step``: (loss [rows], gradient [rows, vocab]) in one launch.  ``out`` may be z itself."""
+    import torch
+    a = _distill_inputs(z, idx, t, tau)
+    _row_floats(weight, z.shape[0], "weight")
+    with _Place(stream, z, idx, t, weight) as at:
+        loss = torch.empty(z.shape[0], dtype=torch.float32, device=z.device)
+        dz = _distill_out(z, out, idx, t, weight)
+        rc = lib.idkm_distill_step(*a, None if weight is None else weight.data_ptr(), loss.data_ptr(), dz.data_ptr(), _ld(dz),
+                                   at.handle)
+    _check(rc)
+    return loss, dz
 
 
 def describe_path(d: int, k: int, adj_max_iter: int = 0, adjoint_method: int = 0) -> dict:

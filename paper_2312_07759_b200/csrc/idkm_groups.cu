@@ -1,0 +1,313 @@
+// Hard assignment with a scale per group of weights: the 4-bit codes and scales one ships where a layer's rows or channels
+// differ in size too much for one codebook.  A group of g consecutive weights of a row gets s = max|w| / max|c|, rounded to the
+// type the scales are kept in, and every weight the codebook entry nearest to it over s:  q(w) = argmin_j |w - s c_j|.
+//
+// Arithmetic.  The codebook is sorted once per block; a weight descends a binary tree of the 15 midpoints with r = w / s, four
+// steps of a subtraction each.  r is off by at most 2^-22 max|c| (one rounding of 1 / s, one of the product, one of a
+// midpoint, |r| <= 2 max|c| or beyond every midpoint), so a weight that passes no midpoint within GROUPS_MARGIN = 2^-20 max|c|
+// has the nearest entry; any other, a few in 10^5, is compared with all entries in fp64, where the products s c_j are exact and
+// ties go to the lowest index.  The result is that of the fp64 comparison for every weight.
+//
+// What bounds it: traffic (W in, half a byte a weight out), as long as a weight costs no more than about 20 instructions.
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include "idkm_types.cuh"
+#include "../../include/idkm.h"
+
+namespace {
+
+using namespace idkm;
+
+constexpr int GROUPS_BLOCK = 256;
+constexpr int GROUPS_LANE = 8;                       // consecutive weights of a lane: its codes are one 32-bit word
+constexpr int GROUPS_WARP = 32 * GROUPS_LANE;        // weights of a warp
+constexpr float GROUPS_MARGIN = 9.5367431640625e-07f;   // 2^-20
+
+struct GroupsParams {
+  const void* W;
+  long long rows, cols, ldw;
+  const void* C;
+  int k;
+  long long group, n_groups;
+  unsigned char* codes;
+  long long pitch;
+  void* scales;
+  void* Wq;
+  int vec_in, vec_out;   // rows of W, of Wq, start on 16-byte boundaries
+};
+
+struct GroupsTable {
+  float c[16];          // the codebook as given; entries that are not finite, and those past k, are NaN
+  float tree[16];       // midpoints of the sorted distinct entries, [0] unused: children of node i are 2 i and 2 i + 1
+  unsigned long long at;   // the index of the entry at each place of the sorted order, 4 bits each
+  float margin, c_max;
+  int zero;             // the code of a weight that is 0: the entry nearest to 0
+  int slow;             // entries so close, or so large or small, that every weight is compared in fp64
+};
+
+// Sorts the codebook by counting.  Called by the whole block.
+template <class T>
+__device__ void groups_table(GroupsTable& t, const void* C, int k) {
+  const int tid = threadIdx.x;
+  const float inf = __int_as_float(0x7f800000), nan = __int_as_float(0x7fc00000);
+  if (tid < 16) {
+    const float x = tid < k ? to_f32(reinterpret_cast<const T*>(C)[tid]) : nan;
+    t.c[tid] = fabsf(x) < inf ? x : nan;
+  }
+  __syncthreads();
+  if (tid < 32) {
+    const float x = tid < 16 ? t.c[tid] : nan;
+    bool kept = x == x;   // the first of equal entries
+    int rank = 0;
+    float most = 0.f;
+    for (int j = 0; j < 16; ++j) {
+      const float y = t.c[j];
+      if (y == y) most = fmaxf(most, fabsf(y));
+      if (y == x && j < tid) kept = false;
+    }
+    const unsigned keepers = __ballot_sync(0xffffffffu, kept);
+    for (int j = 0; j < 16; ++j)
+      if ((keepers >> j & 1u) && t.c[j] < x) ++rank;
+    // place `rank` of the sorted order; the next larger kept entry
+    float up = inf;
+    for (int j = 0; j < 16; ++j)
+      if ((keepers >> j & 1u) && t.c[j] > x) up = fminf(up, t.c[j]);
+    const float mid = up < inf ? 0.5f * x + 0.5f * up : inf;   // above the place; inf above the last one
+    const bool close = kept && up < inf && !(up - x > 1e-12f * most);
+    const int slow = __any_sync(0xffffffffu, close) || !(most > 8.6736174e-19f && most < 1.1529215e18f);   // 2^-60, 2^60
+    unsigned lo = 0u, hi = 0u;
+    if (kept) {
+      if (rank < 8) lo = (unsigned)tid << (4 * rank);
+      else hi = (unsigned)tid << (4 * (rank - 8));
+    }
+    lo = __reduce_or_sync(0xffffffffu, lo);
+    hi = __reduce_or_sync(0xffffffffu, hi);
+    if (tid < 16) t.tree[tid] = inf;
+    // (a codebook symmetric about 0 has a midpoint there, and a pruned layer many weights on it)
+    const unsigned size = kept ? __float_as_uint(x) & 0x7fffffffu : 0xffffffffu, least = __reduce_min_sync(0xffffffffu, size);
+    const int zero = (int)__reduce_min_sync(0xffffffffu, kept && size == least ? (unsigned)tid : 31u) & 15;
+    __syncwarp();
+    // the midpoint above place p (0..14) is the node that separates p from p + 1: in-order position p of a tree of 15
+    if (kept && rank < 15) {
+      const int p = rank + 1, low = __ffs(p) - 1;          // p = odd * 2^low, at depth 3 - low
+      t.tree[(1 << (3 - low)) + (p >> (low + 1))] = mid;
+    }
+    if (tid == 0) {
+      t.at = (unsigned long long)hi << 32 | lo;
+      t.margin = GROUPS_MARGIN * most;
+      t.c_max = most;
+      t.slow = slow;
+      t.zero = zero;
+    }
+  }
+  __syncthreads();
+}
+
+__device__ __noinline__ int groups_exact(const GroupsTable& t, float w, float s) {
+  double best = 1.0 / 0.0;
+  int at = 0;
+  for (int j = 0; j < 16; ++j) {
+    const double d = fabs((double)w - (double)s * (double)t.c[j]);
+    if (d < best) {   // (a NaN is never nearer)
+      best = d;
+      at = j;
+    }
+  }
+  return at;
+}
+
+// s = max|w| / max|c| as the scales' type holds it, and the factor to look weights up by (0: the group needs the exact form).
+template <class T>
+__device__ __forceinline__ T groups_scale(const GroupsTable& t, unsigned most_bits, float& s, float& inv) {
+  const T held = from_f32<T>(t.c_max > 0.f ? __fdiv_rn(__uint_as_float(most_bits), t.c_max) : 0.f);
+  s = to_f32(held);
+  inv = (!t.slow && s > 7.8886091e-31f && s < 1.2676506e30f) ? __fdiv_rn(1.f, s) : 0.f;   // 2^-100, 2^100
+  return held;
+}
+
+// The codes of a lane's eight weights.
+__device__ __forceinline__ unsigned groups_codes(const GroupsTable& t, const float (&w)[GROUPS_LANE], float s, float inv) {
+  unsigned out = 0u;
+  float near[GROUPS_LANE];
+  unsigned node[GROUPS_LANE];
+#pragma unroll
+  for (int e = 0; e < GROUPS_LANE; ++e) {
+    node[e] = 1u;
+    near[e] = __int_as_float(0x7f800000);
+  }
+#pragma unroll
+  for (int level = 0; level < 4; ++level)
+#pragma unroll
+    for (int e = 0; e < GROUPS_LANE; ++e) {
+      const float d = __fmaf_rn(w[e], inv, -t.tree[node[e]]);   // (one rounding less than a product and a difference)
+      near[e] = fminf(near[e], fabsf(d));
+      node[e] = __funnelshift_l(~__float_as_uint(d), node[e], 1);   // 2 node + (r at or above the midpoint)
+    }
+#pragma unroll
+  for (int e = 0; e < GROUPS_LANE; ++e) out |= ((unsigned)(t.at >> (4u * (node[e] & 15u))) & 15u) << (4 * e);
+  float least = near[0];
+#pragma unroll
+  for (int e = 1; e < GROUPS_LANE; ++e) least = fminf(least, near[e]);
+  if (!(least > t.margin) || inv == 0.f) {
+    const bool finite = fabsf(s) < __int_as_float(0x7f800000);
+#pragma unroll
+    for (int e = 0; e < GROUPS_LANE; ++e)
+      if (!(near[e] > t.margin) || inv == 0.f)
+        out = (out & ~(15u << (4 * e))) | (unsigned)(!finite || s == 0.f ? 0 : w[e] == 0.f ? t.zero : groups_exact(t, w[e], s)) << (4 * e);
+  }
+  return out;
+}
+
+// Eight weights of a row from column c on; zeros past its end.
+template <class TW>
+__device__ __forceinline__ void groups_load(const TW* row, long long c, long long cols, int vec, float (&w)[GROUPS_LANE]) {
+  if (vec && c + GROUPS_LANE <= cols) {
+    constexpr int N = Vec16<TW>::N;
+#pragma unroll
+    for (int q = 0; q < GROUPS_LANE / N; ++q) {
+      Vec16<TW> x;
+      x.raw = __ldg(reinterpret_cast<const uint4*>(row + c) + q);
+#pragma unroll
+      for (int e = 0; e < N; ++e) w[q * N + e] = to_f32(x.e[e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < GROUPS_LANE; ++e) w[e] = c + e < cols ? to_f32(row[c + e]) : 0.f;
+  }
+}
+
+template <class TW>
+__device__ __forceinline__ void groups_store_wq(const GroupsTable& t, TW* row, long long c, long long cols, int vec, unsigned codes, float s) {
+  float q[GROUPS_LANE];
+#pragma unroll
+  for (int e = 0; e < GROUPS_LANE; ++e) q[e] = s * t.c[codes >> (4 * e) & 15u];
+  if (vec && c + GROUPS_LANE <= cols) {
+    constexpr int N = Vec16<TW>::N;
+#pragma unroll
+    for (int v = 0; v < GROUPS_LANE / N; ++v) {
+      Vec16<TW> x;
+#pragma unroll
+      for (int e = 0; e < N; ++e) x.e[e] = from_f32<TW>(q[v * N + e]);
+      reinterpret_cast<uint4*>(row + c)[v] = x.raw;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < GROUPS_LANE; ++e)
+      if (c + e < cols) row[c + e] = from_f32<TW>(q[e]);
+  }
+}
+
+// Codes of the weights past a row's end are 0.
+__device__ __forceinline__ unsigned groups_keep(unsigned codes, long long c, long long cols) {
+  return c + GROUPS_LANE <= cols ? codes : c >= cols ? 0u : codes & ((1u << (4 * (int)(cols - c))) - 1u);
+}
+
+__device__ __forceinline__ unsigned groups_bits(const float (&w)[GROUPS_LANE]) {
+  unsigned most = 0u;   // |w| by its bits: ordered like the values, infinities above them, NaN above those
+#pragma unroll
+  for (int e = 0; e < GROUPS_LANE; ++e) most = max(most, __float_as_uint(w[e]) & 0x7fffffffu);
+  return most;
+}
+
+// Groups of 32, 64, 128 or 256 weights: L = g / 8 neighbouring lanes share one.
+template <class TW, class T>
+__global__ void __launch_bounds__(GROUPS_BLOCK) idkm_groups_short(const GroupsParams p) {
+  __shared__ GroupsTable t;
+  groups_table<T>(t, p.C, p.k);
+  const int lane = threadIdx.x & 31, L = (int)(p.group / GROUPS_LANE);
+  const long long per_row = (p.cols + GROUPS_WARP - 1) / GROUPS_WARP, total = p.rows * per_row;
+  const long long n_warps = (long long)gridDim.x * (GROUPS_BLOCK / 32);
+  for (long long i = (long long)blockIdx.x * (GROUPS_BLOCK / 32) + (threadIdx.x >> 5); i < total; i += n_warps) {
+    const long long row = i / per_row, c = (i % per_row) * GROUPS_WARP + lane * GROUPS_LANE;
+    float w[GROUPS_LANE];
+    groups_load(reinterpret_cast<const TW*>(p.W) + row * p.ldw, c, p.cols, p.vec_in, w);
+    unsigned most = groups_bits(w);
+    for (int o = 1; o < L; o <<= 1) most = max(most, __shfl_xor_sync(0xffffffffu, most, o));
+    float s, inv;
+    const T held = groups_scale<T>(t, most, s, inv);
+    const unsigned codes = groups_keep(groups_codes(t, w, s, inv), c, p.cols);
+    if (c < p.cols) {
+      if (lane % L == 0) reinterpret_cast<T*>(p.scales)[row * p.n_groups + c / p.group] = held;
+      if (p.Wq) groups_store_wq(t, reinterpret_cast<TW*>(p.Wq) + row * p.cols, c, p.cols, p.vec_out, codes, s);
+    }
+    if (c < 2 * p.pitch) *reinterpret_cast<unsigned*>(p.codes + row * p.pitch + c / 2) = codes;
+  }
+}
+
+// Longer groups: a block each, which reads the group twice (the second time from L2).
+template <class TW, class T>
+__global__ void __launch_bounds__(GROUPS_BLOCK) idkm_groups_long(const GroupsParams p) {
+  __shared__ GroupsTable t;
+  __shared__ unsigned part[GROUPS_BLOCK / 32];
+  groups_table<T>(t, p.C, p.k);
+  for (long long i = blockIdx.x; i < p.rows * p.n_groups; i += gridDim.x) {
+    const long long row = i / p.n_groups, g = i % p.n_groups, begin = g * p.group;
+    const long long end = min(begin + p.group, p.cols), end_codes = g + 1 == p.n_groups ? 2 * p.pitch : end;
+    const TW* wr = reinterpret_cast<const TW*>(p.W) + row * p.ldw;
+    unsigned most = 0u;
+    for (long long c = begin + threadIdx.x * GROUPS_LANE; c < end; c += GROUPS_BLOCK * GROUPS_LANE) {
+      float w[GROUPS_LANE];
+      groups_load(wr, c, end, p.vec_in, w);
+      most = max(most, groups_bits(w));
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = most;
+    __syncthreads();
+    most = 0u;
+#pragma unroll
+    for (int q = 0; q < GROUPS_BLOCK / 32; ++q) most = max(most, part[q]);
+    __syncthreads();
+    float s, inv;
+    const T held = groups_scale<T>(t, most, s, inv);
+    if (threadIdx.x == 0) reinterpret_cast<T*>(p.scales)[i] = held;
+    for (long long c = begin + threadIdx.x * GROUPS_LANE; c < end_codes; c += GROUPS_BLOCK * GROUPS_LANE) {
+      float w[GROUPS_LANE];
+      groups_load(wr, c, end, p.vec_in, w);
+      const unsigned codes = groups_keep(groups_codes(t, w, s, inv), c, end);
+      if (p.Wq) groups_store_wq(t, reinterpret_cast<TW*>(p.Wq) + row * p.cols, c, end, p.vec_out, codes, s);
+      *reinterpret_cast<unsigned*>(p.codes + row * p.pitch + c / 2) = codes;
+    }
+  }
+}
+
+}  // namespace
+
+extern "C" int64_t idkm_group_codes_pitch(int64_t cols) { return cols < 1 ? 0 : (cols + 31) / 32 * 16; }
+
+extern "C" int idkm_assign_groups(const void* W, int w_type, int64_t rows, int64_t cols, int64_t ldw, const void* C, int k, int type,
+                                  int64_t group, unsigned char* codes_out, void* scales_out, void* Wq_out, void* cuda_stream) {
+  if (!W || !C || !codes_out || !scales_out) return IDKM_ERR_NULL;
+  if (k < 1 || k > 16 || !elem_known(w_type) || !elem_known(type)) return IDKM_ERR_UNSUPPORTED;
+  if (rows < 1 || cols < 1 || ldw < cols || group < 1 || cols > (INT64_C(1) << 50) / rows) return IDKM_ERR_SHAPE;
+  if (group < cols && group != 32 && group != 64 && group % 128 != 0) return IDKM_ERR_UNSUPPORTED;
+  if (Wq_out == W || Wq_out == (void*)codes_out || Wq_out == scales_out) return IDKM_ERR_PARAM;
+  const int wb = elem_bytes(w_type), tb = elem_bytes(type);
+  if (((uintptr_t)W | (uintptr_t)Wq_out) % wb || ((uintptr_t)C | (uintptr_t)scales_out) % tb || (uintptr_t)codes_out % 16) return IDKM_ERR_ALIGN;
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms < 1)
+    return IDKM_ERR_CUDA;
+  GroupsParams p;
+  p.W = W; p.rows = rows; p.cols = cols; p.ldw = ldw; p.C = C; p.k = k;
+  p.pitch = idkm_group_codes_pitch(cols);
+  // one scale per row: a group that ends with the row (32 codes at a time are kept whole)
+  p.group = group >= cols ? (cols <= 32 ? 32 : cols <= 64 ? 64 : (cols + 127) / 128 * 128) : group;
+  p.n_groups = (cols + p.group - 1) / p.group;
+  p.codes = codes_out; p.scales = scales_out; p.Wq = Wq_out;
+  p.vec_in = (uintptr_t)W % 16 == 0 && ldw * wb % 16 == 0;
+  p.vec_out = (uintptr_t)Wq_out % 16 == 0 && cols * wb % 16 == 0;
+  const bool shorter = p.group <= GROUPS_WARP && GROUPS_WARP % p.group == 0;
+  const long long per_row = (cols + GROUPS_WARP - 1) / GROUPS_WARP;
+  const long long jobs = shorter ? (rows * per_row + GROUPS_BLOCK / 32 - 1) / (GROUPS_BLOCK / 32) : rows * p.n_groups;
+  const int grid = (int)(jobs < (long long)sms * 8 ? jobs : (long long)sms * 8);
+  cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
+  return with_type(w_type, [&](auto* w) {
+    return with_type(type, [&](auto* c) {
+      using TW = std::remove_pointer_t<decltype(w)>;
+      using T = std::remove_pointer_t<decltype(c)>;
+      if (shorter) idkm_groups_short<TW, T><<<grid, GROUPS_BLOCK, 0, st>>>(p);
+      else idkm_groups_long<TW, T><<<grid, GROUPS_BLOCK, 0, st>>>(p);
+      return cudaGetLastError() == cudaSuccess ? IDKM_OK : IDKM_ERR_CUDA;
+    });
+  });
+}
