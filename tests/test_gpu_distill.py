@@ -4,7 +4,9 @@ Tolerances.  Exponents x = z / tau are off by one rounding, 2^-24 |x|, and ln q 
 X the largest |x| of a row (finite ones), an exponential or a normaliser is off by at most e = (4 X + 32) 2^-24 of its value
 (the 32: the functions' own 2 ulp and the joins of sums).  The loss is a sum of p (ln p - ln q) with p off by e and either
 logarithm off by e: tau^2 ((sum p |ln p - ln q|) e + 2 e), rounded once.  The gradient is w tau (q - p): w tau (q + p) e, then
-the rounding to its type, eps / 2 of its value (and half the least fp16 step)."""
+the rounding to its type, eps / 2 of its value (and half the least fp16 step).  Exponentials below the normal range are 0: an
+exponential is taken relative to a largest one, whose share of the row is at most 1, in up to two factors, either of which is
+0 only where it is below 2^-126 and the other at most 1; so q is off by at most 2^-126 more, and the gradient by w tau 2^-126."""
 import numpy as np
 import pytest
 
@@ -42,7 +44,7 @@ def _reference(z, idx, t, tau, w):
     mass = np.exp(lq)
     for r in range(p.shape[0]):
         np.add.at(mass[r], I[r], p[r])
-    return loss, ltol, dz, mass * (w64 * tau * e)[:, None]
+    return loss, ltol, dz, mass * (w64 * tau * e)[:, None] + (w64 * tau * 2.0 ** -126)[:, None]
 
 
 def _check(torch, got_loss, got_dz, ref):
