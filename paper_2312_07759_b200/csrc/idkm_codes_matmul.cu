@@ -1,7 +1,9 @@
-// Products with 4-bit weights and group scales: Y[m][n] = sum_k s[n][k / g] C[code[n][k]] X[m][k].
+// Products with 4-bit weights and group scales: Y[m][n] = sum_k s[n][k / g] C[code[n][k]] X[m][k], for few rows of X.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
+#include <type_traits>
+#include "idkm_per_device.h"
 #include "idkm_types.cuh"
 #include "../../include/idkm.h"
 
@@ -81,6 +83,422 @@ __global__ void __launch_bounds__(ROWS_BLOCK) idkm_codes_rows(const CodesParams 
   }
 }
 
+// ---- a few rows of X in 16-bit types ------------------------------------------------------------------------------------
+// A pair of codes, one byte, is looked up in a table of the 256 pairs of codebook entries, and the pairs are the operands of matrix
+// products over 16 rows of W: no conversion, no multiplication of single weights, and the sums of all columns in fp32.
+//
+// Which column of X a product's k-th place holds is free as long as both operands agree, so a thread takes 32 neighbouring codes
+// of two rows as they lie in memory (16 bytes each): the four threads that share a row cover 128 columns, a "strip".  The table
+// has a copy for every lane (a word of each of the 32 banks), so that 32 lanes look 32 different pairs up in one cycle: 64
+// weights a cycle of a multiprocessor, 9 TB/s of codes, above what memory delivers.  Its rows are 256 bytes apart and it lies on a
+// multiple of 64 KB, so that an address is four bytes put together by one instruction: two of the table's, the pair, the lane's.
+// (Rows of 128 bytes, a shift and a mask a pair: 57 us where this takes 27, one token through 28672 x 8192.)
+//
+// The scale multiplies the group's fp32 sum.  Where a strip has Q = 2 or 4 groups, the threads of a row exchange words first (a
+// transposition by shuffles), so that all four work on one group at a time.
+//
+// One block a multiprocessor takes its share of the tiles of 16 rows, a batch of tiles at a time.  The batch's chunks of two strips,
+// one after another, go to its 16 warps in turn, so that the block reads pieces of rows that lie together.  A warp of its own has
+// them copied into shared memory, 16 chunks a stage, two or three stages ahead (loads into registers two steps ahead were
+// waited for wherever the loop branches: 41 to 52 us).  The warps' sums of a batch meet in shared memory (in the halves of the table's
+// rows that are free) in a fixed order, its scales come while the batch before is worked on, X lies there in the order the
+// threads read it.
+constexpr int FEW_WARPS = 16, FEW_BLOCK = 32 * FEW_WARPS, FEW_ROWS = 16;
+constexpr int FEW_STRIPS = 2, FEW_CHUNK = 128 * FEW_STRIPS;
+constexpr int FEW_PITCH = FEW_WARPS * (FEW_CHUNK / 2) + 64, FEW_STAGE = FEW_ROWS * FEW_PITCH;   // (two rows' 64 bytes in different banks)
+constexpr int FEW_TABLE = 64 * 1024, FEW_SMEM = 227 * 1024 - 256, FEW_TILES = 16;               // tiles of a batch, at most
+constexpr int FEW_BEFORE = FEW_TABLE - 1024, FEW_AFTER = FEW_SMEM - FEW_BEFORE - FEW_TABLE;     // shared memory starts at 1 KB
+constexpr int FEW_POLLS = 1 << 22;   // (each waits for some time itself)
+
+__device__ __forceinline__ void few_mma(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1, __nv_bfloat16*) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void few_mma(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1, __half*) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void few_mma(float (&)[4], const unsigned (&)[4], unsigned, unsigned, float*) {}
+
+__device__ __forceinline__ float few_scale(unsigned short u, __nv_bfloat16*) { return __uint_as_float((unsigned)u << 16); }
+__device__ __forceinline__ float few_scale(unsigned short u, __half*) { return __half2float(__ushort_as_half(u)); }
+
+// Eight 16-bit elements of a row from column k on, zeros past its end, whatever the row's alignment: from the one or two
+// 16-byte words that hold them.  (A word that holds one byte of the row lies in the row's pages.)
+__device__ __forceinline__ uint4 few_load8(const void* row, long long k, long long cols) {
+  uint4 r = make_uint4(0u, 0u, 0u, 0u);
+  if (k >= cols) return r;
+  const uintptr_t at = (uintptr_t)row + 2 * k, end = (uintptr_t)row + 2 * cols;
+  const uint4* word = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+  const unsigned off = (unsigned)(at & 15u);
+  r = __ldg(word);
+  if (off) {
+    uint4 h = make_uint4(0u, 0u, 0u, 0u);
+    if ((uintptr_t)(word + 1) < end) h = __ldg(word + 1);
+    unsigned w[8] = {r.x, r.y, r.z, r.w, h.x, h.y, h.z, h.w};
+    if (off & 8u) { w[0] = w[2]; w[1] = w[3]; w[2] = w[4]; w[3] = w[5]; w[4] = w[6]; w[5] = w[7]; }
+    if (off & 4u) { w[0] = w[1]; w[1] = w[2]; w[2] = w[3]; w[3] = w[4]; w[4] = w[5]; }
+    if (off & 2u) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+    r = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  if (k + 8 > cols) {
+    const int keep = (int)(cols - k);   // 1 to 7 elements
+    r.x &= keep >= 2 ? ~0u : 0xffffu;
+    r.y &= keep >= 4 ? ~0u : keep == 3 ? 0xffffu : 0u;
+    r.z &= keep >= 6 ? ~0u : keep == 5 ? 0xffffu : 0u;
+    r.w &= keep == 7 ? 0xffffu : 0u;
+  }
+  return r;
+}
+
+// Words w[q] of threads t = 0..3 of a quad: Q = 4: thread t gets word t of thread q's; Q = 2: of the threads with q / 2 = t / 2 words
+// 2 (t % 2) and 2 (t % 2) + 1 -- so that w[q] of the whole quad belongs to group q Q / 4 of the chunk.
+template <int Q>
+__device__ __forceinline__ void few_exchange(uint4& w, int tig) {
+  if constexpr (Q >= 2) {   // halves between threads t and t ^ 2
+    const bool up = tig & 2;
+    const unsigned a = __shfl_xor_sync(0xffffffffu, up ? w.x : w.z, 2), b = __shfl_xor_sync(0xffffffffu, up ? w.y : w.w, 2);
+    if (up) { w.x = a; w.y = b; }
+    else { w.z = a; w.w = b; }
+  }
+  if constexpr (Q == 4) {   // words between threads t and t ^ 1
+    const bool up = tig & 1;
+    const unsigned a = __shfl_xor_sync(0xffffffffu, up ? w.x : w.y, 1), b = __shfl_xor_sync(0xffffffffu, up ? w.z : w.w, 1);
+    if (up) { w.x = a; w.z = b; }
+    else { w.y = a; w.w = b; }
+  }
+}
+// The columns, by eights within a chunk, that w[q] of thread t then stands for.
+template <int Q>
+__host__ __device__ __forceinline__ constexpr int few_column(int q, int t) {
+  // word j of thread s stands for eight 4 s + j
+  return Q == 1 ? 4 * t + q : Q == 2 ? 4 * ((q & 2) + (t & 1)) + (t & 2) + (q & 1) : 4 * q + t;
+}
+
+__device__ __forceinline__ bool few_wait(unsigned bar, unsigned parity) {
+  for (int i = 0; i < FEW_POLLS; ++i) {
+    unsigned done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+__device__ __forceinline__ void few_arrive(unsigned bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+// How a product is taken: tiles of a batch, stages of codes, words of a row's scales in shared memory (odd: a bank a row), bytes of
+// a row of X there (two rows' 64 bytes in different banks).
+struct FewPlan {
+  int chunks, tiles, stages, scale_words, xs;
+  unsigned per_group;   // strip * per_group >> 20 is the group of a strip, where groups have whole strips (strips and a group's strips below 2^9)
+  __host__ __device__ int scale_bytes() const { return 2 * tiles * FEW_ROWS * scale_words * 4; }   // of two batches
+  __host__ __device__ int parts() const { return chunks < FEW_WARPS ? chunks : FEW_WARPS; }        // sums of a tile that meet
+};
+
+// The i-th 16 of the sums that meet, in the free halves of the table's rows.
+__device__ __forceinline__ float* few_sums(unsigned char* table, int i) { return reinterpret_cast<float*>(table + (i >> 1) * 256 + 128 + (i & 1) * 64); }
+
+template <class T, int Q, int NT, bool SCALED>
+__global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid_constant__ CodesParams p, const __grid_constant__ FewPlan f) {
+  T* const type = nullptr;
+  extern __shared__ __align__(16) unsigned char few_raw[];
+  __shared__ __align__(8) unsigned long long s_bar[2][4];   // a stage's codes are there; all warps have read them
+  const unsigned raw = (unsigned)__cvta_generic_to_shared(few_raw), table = (raw + FEW_TABLE - 1) & ~(unsigned)(FEW_TABLE - 1);
+  const unsigned stage0 = table + FEW_TABLE, full = (unsigned)__cvta_generic_to_shared(s_bar), empty = full + 32;
+  unsigned char* const at_table = few_raw + (table - raw);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, gid = lane >> 2, tig = lane & 3;
+  const int chunks = f.chunks, tokens = (int)p.tokens;
+  const int before = min(((int)(table - raw) - f.scale_bytes()) / f.xs, tokens);   // rows of X that lie before the table
+  auto row_of = [&](int m) { return m < before ? few_raw + f.scale_bytes() + m * f.xs : at_table + FEW_TABLE + f.stages * FEW_STAGE + (m - before) * f.xs; };
+  const int code_bytes = (int)((p.cols + 31) / 32) * 16;
+  const int n_tiles = (int)((p.rows + FEW_ROWS - 1) / FEW_ROWS), n_groups = (int)p.n_groups;
+  const int tile0 = (int)((long long)n_tiles * blockIdx.x / gridDim.x), tile1 = (int)((long long)n_tiles * (blockIdx.x + 1) / gridDim.x);
+
+  if (tid < 2 * f.stages) {
+    const int s = tid >> 1;
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"((tid & 1 ? empty : full) + 8 * s), "r"(tid & 1 ? FEW_WARPS : FEW_ROWS) : "memory");
+  }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  // the codebook is asked for first
+  const unsigned short* c = reinterpret_cast<const unsigned short*>(p.C);
+  unsigned lo = 0u, hi = 0u;
+  if (tid < 256) {
+    if ((tid & 15) < p.k) lo = __ldg(c + (tid & 15));
+    if ((tid >> 4) < p.k) hi = __ldg(c + (tid >> 4));
+  }
+  __syncthreads();
+
+  if (warp == FEW_WARPS) {   // the copies: a lane a row
+    if (lane < FEW_ROWS) {
+      int stage = 0, turn = 0;
+      bool filled = false;   // every stage has been filled once
+      for (int batch = tile0; batch < tile1; batch += f.tiles) {
+        const int steps = min(f.tiles, tile1 - batch) * chunks;
+        int tile = batch, chunk = 0;
+        for (int s = 0; s < steps; s += FEW_WARPS) {
+          const unsigned bar = full + 8 * stage;
+          if (filled && !few_wait(empty + 8 * stage, (turn & 1) ^ 1)) return;
+          unsigned to = stage0 + stage * FEW_STAGE + lane * FEW_PITCH;
+          for (int left = min(FEW_WARPS, steps - s); left > 0;) {
+            const int n = min(left, chunks - chunk);
+            const long long row = (long long)tile * FEW_ROWS + lane;
+            const int bytes = min(n * (FEW_CHUNK / 2), code_bytes - chunk * (FEW_CHUNK / 2));
+            if (row < p.rows) {   // (what is not copied is what was there: codes of rows or columns past the last count for nothing)
+              asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+              asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                           ::"r"(to), "l"(p.codes + row * p.pitch + chunk * (FEW_CHUNK / 2)), "r"(bytes), "r"(bar) : "memory");
+            }
+            to += n * (FEW_CHUNK / 2);
+            left -= n;
+            chunk += n;
+            if (chunk == chunks) {
+              chunk = 0;
+              ++tile;
+            }
+          }
+          few_arrive(bar);
+          if (++stage == f.stages) {
+            stage = 0;
+            turn ^= 1;
+            filled = true;
+          }
+        }
+      }
+    }
+    return;
+  }
+
+  // scales of a batch, by words; a row's may begin in the middle of one.  (A word that holds one byte of them lies in their pages.)
+  auto copy_scales = [&](int batch, int turn) {
+    const long long r0 = (long long)batch * FEW_ROWS, rows = min((long long)min(batch + f.tiles, tile1) * FEW_ROWS, p.rows) - r0;
+    const unsigned to = raw + (unsigned)(turn * (f.scale_bytes() / 2));
+    for (int r = warp; r < (int)rows; r += FEW_WARPS) {
+      const uintptr_t at = (uintptr_t)p.scales + 2 * (r0 + r) * p.n_groups;
+      for (uintptr_t word = (at & ~(uintptr_t)3) + 4 * lane, place = to + (r * f.scale_words + lane) * 4; word < at + 2 * n_groups; word += 128, place += 128)
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((unsigned)place), "l"(word) : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  if (SCALED) copy_scales(tile0, 0);
+  const int words = chunks * (FEW_CHUNK / 8), n_words = tokens * words;   // 16-byte words of a row of X
+  auto place_x = [&](int i, bool load, uint4& x) {
+    const int m = i / words, v = i - m * words, place = v & 15;   // place 4 q + t of a strip: for word q of thread t
+    if (load) x = few_load8(reinterpret_cast<const T*>(p.X) + m * p.ldx, (long long)(v >> 4) * 128 + 8 * few_column<Q>(place >> 2, place & 3), p.cols);
+    else *reinterpret_cast<uint4*>(row_of(m) + v * 16) = x;
+  };
+  {
+    uint4 first[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (tid + u * FEW_BLOCK < n_words) place_x(tid + u * FEW_BLOCK, true, first[u]);
+    if (tid < 256) {
+      const unsigned both = lo | hi << 16;
+#pragma unroll
+      for (int q = 0; q < 8; ++q)   // (lanes at different places of their rows: in different banks)
+        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(table + tid * 256 + ((q + lane) & 7) * 16), "r"(both) : "memory");
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+      if (tid + u * FEW_BLOCK < n_words) place_x(tid + u * FEW_BLOCK, false, first[u]);
+  }
+  for (int i = tid + 2 * FEW_BLOCK; i < n_words; i += 4 * FEW_BLOCK) {
+    uint4 some[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i + u * FEW_BLOCK < n_words) place_x(i + u * FEW_BLOCK, true, some[u]);
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (i + u * FEW_BLOCK < n_words) place_x(i + u * FEW_BLOCK, false, some[u]);
+  }
+  auto meet = [] { asm volatile("bar.sync 1, %0;" ::"n"(FEW_BLOCK) : "memory"); };
+  asm volatile("cp.async.wait_group 0;" ::: "memory");
+  meet();
+
+  // (a value that is there after the barrier only: the lookups, which may be moved about, stay behind it)
+  unsigned mine;
+  asm volatile("or.b32 %0, %1, %2;" : "=r"(mine) : "r"(table), "r"((unsigned)lane * 4u) : "memory");
+  // this thread's row of X; threads of columns that X has no row for keep their zeros
+  unsigned x_row[NT], x_there[NT];
+  uint4 x[2][NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    x_there[n] = n * 8 + gid < tokens;
+    x_row[n] = (unsigned)__cvta_generic_to_shared(row_of(min(n * 8 + gid, tokens - 1))) + tig * 16;
+    x[0][n] = x[1][n] = make_uint4(0u, 0u, 0u, 0u);
+  }
+  auto first_scale = [&](int strip) { return Q > 1 ? strip * Q : (int)((unsigned)strip * f.per_group >> 20); };
+  const int parts = f.parts(), batch_sums = f.tiles * parts * tokens;
+  const unsigned my_codes = stage0 + gid * FEW_PITCH + warp * (FEW_CHUNK / 2) + tig * 16;
+  int stage = 0, stage_turn = 0, turn = 0;
+  bool lost = false;   // a wait ran out (none does: the copies wait for nothing but these warps); later ones do not wait
+  float tot[NT][4];
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tot[n][i] = 0.f;
+  for (int batch = tile0; batch < tile1; batch += f.tiles, turn ^= 1) {
+    if (SCALED) copy_scales(batch + f.tiles, turn ^ 1);
+    const int n_batch = min(f.tiles, tile1 - batch), steps = n_batch * chunks;
+    int tile = warp / chunks, chunk = warp % chunks;   // of the batch
+    for (int s = 0; s < steps; s += FEW_WARPS) {
+      if (!lost) lost = !few_wait(full + 8 * stage, stage_turn);
+      uint4 w[FEW_STRIPS][2];
+#pragma unroll
+      for (int u = 0; u < FEW_STRIPS; ++u)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[u][h].x), "=r"(w[u][h].y), "=r"(w[u][h].z), "=r"(w[u][h].w)
+                       : "r"(my_codes + stage * FEW_STAGE + h * 8 * FEW_PITCH + u * 64));
+      if (s + warp < steps) {
+        float acc[NT][4];
+        if (SCALED) {
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[n][i] = 0.f;
+        }
+        const int x_at = chunk * (2 * FEW_CHUNK);
+        unsigned scale_of[2];   // the scales of this thread's rows
+        if (SCALED) {
+          const int r = tile * FEW_ROWS + gid;
+          const unsigned odd = (unsigned)(((uintptr_t)p.scales >> 1) + ((long long)batch * FEW_ROWS + r) * n_groups) & 1u;   // (8 rows on: the same)
+          scale_of[0] = raw + (unsigned)(turn * (f.scale_bytes() / 2) + r * f.scale_words * 4) + 2 * odd;
+          scale_of[1] = scale_of[0] + 8 * f.scale_words * 4;
+        }
+#pragma unroll
+        for (int u = 0; u < FEW_STRIPS; ++u) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) few_exchange<Q>(w[u][h], tig);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+              asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t@p ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
+                           : "+r"(x[q & 1][n].x), "+r"(x[q & 1][n].y), "+r"(x[q & 1][n].z), "+r"(x[q & 1][n].w)
+                           : "r"(x_row[n] + x_at + u * 256 + q * 64), "r"(x_there[n]));
+            const unsigned w0 = q == 0 ? w[u][0].x : q == 1 ? w[u][0].y : q == 2 ? w[u][0].z : w[u][0].w;
+            const unsigned w1 = q == 0 ? w[u][1].x : q == 1 ? w[u][1].y : q == 2 ? w[u][1].z : w[u][1].w;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+              unsigned a[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                // (the lane's byte, byte 2 j + i / 2 of the codes, the table's two)
+                const unsigned at = __byte_perm(mine, i & 1 ? w1 : w0, 0x3240u + 0x10u * (unsigned)(2 * j + i / 2));
+                asm("ld.shared.u32 %0, [%1];" : "=r"(a[i]) : "r"(at));
+              }
+#pragma unroll
+              for (int n = 0; n < NT; ++n) few_mma(SCALED ? acc[n] : tot[n], a, j ? x[q & 1][n].z : x[q & 1][n].x, j ? x[q & 1][n].w : x[q & 1][n].y, type);
+            }
+            if (SCALED && (q + 1) % (4 / Q) == 0) {   // a group, or a strip, is done
+              const int g = first_scale(chunk * FEW_STRIPS + u) + (Q > 1 ? q * Q / 4 : 0);
+              float sc[2];
+#pragma unroll
+              for (int h = 0; h < 2; ++h) {   // (past the last group only where the codes are past the last column too)
+                unsigned short v = 0;
+                if (g < n_groups) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(scale_of[h] + 2 * g));
+                sc[h] = few_scale(v, type);
+              }
+#pragma unroll
+              for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  tot[n][i] = fmaf(sc[i / 2], acc[n][i], tot[n][i]);
+                  acc[n][i] = 0.f;
+                }
+            }
+          }
+        }
+        const int here = tile, part = chunks < FEW_WARPS ? chunk : warp;
+        chunk += FEW_WARPS;
+        while (chunk >= chunks) {
+          chunk -= chunks;
+          ++tile;
+        }
+        if (tile != here) {   // the warp's part of the tile is done
+          const int base = turn * batch_sums + (here * parts + part) * tokens + 2 * tig;
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            if (n * 8 + 2 * tig < tokens) {
+              float* to = few_sums(at_table, base + n * 8) + gid;
+              to[0] = tot[n][0];
+              to[8] = tot[n][2];
+            }
+            if (n * 8 + 2 * tig + 1 < tokens) {
+              float* to = few_sums(at_table, base + n * 8 + 1) + gid;
+              to[0] = tot[n][1];
+              to[8] = tot[n][3];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tot[n][i] = 0.f;
+          }
+        }
+      }
+      // (the codes have been used, so they have been read)
+      __syncwarp();
+      if (lane == 0) few_arrive(empty + 8 * stage);
+      if (++stage == f.stages) {
+        stage = 0;
+        stage_turn ^= 1;
+      }
+    }
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    meet();   // the batch is done, the next one's scales are there
+    const int n = n_batch * FEW_ROWS;
+    for (int o = tid; o < n * tokens; o += FEW_BLOCK) {
+      const int m = o / n, r = o - m * n;
+      const int base = turn * batch_sums + (r / FEW_ROWS) * parts * tokens + m;
+      float v = 0.f;
+      for (int i = 0; i < parts; ++i) v += few_sums(at_table, base + i * tokens)[r % FEW_ROWS];
+      const long long row = (long long)batch * FEW_ROWS + r;
+      if (row < p.rows) reinterpret_cast<T*>(p.Y)[m * p.ldy + row] = from_f32<T>(lost ? __int_as_float(0x7fc00000) : v);
+    }
+  }
+}
+
+// The plan of a product, false where it does not fit: X and two batches' scales in shared memory before the table and after it, the
+// stages after it, the batches' sums in the table's free halves.
+inline bool few_plan(const CodesParams& p, FewPlan& f) {
+  if (p.tokens > 16 || p.rows > INT32_MAX - FEW_ROWS || p.cols > FEW_AFTER / 2) return false;
+  f.chunks = (int)((p.cols + FEW_CHUNK - 1) / FEW_CHUNK);
+  f.xs = f.chunks * (2 * FEW_CHUNK) + 64;
+  if (p.group >= 128) {
+    const long long per = p.group / 128;   // (longer than a row: one group)
+    if (2 * f.chunks >= 512) return false;
+    f.per_group = per >= 512 ? 0u : (unsigned)(((1 << 20) + per - 1) / per);
+  }
+  f.scale_words = p.scales ? (int)(p.n_groups / 2 + 1) | 1 : 0;
+  for (f.stages = 3; f.stages >= 2; --f.stages)
+    for (f.tiles = FEW_TILES; f.tiles >= 1; f.tiles /= 2) {
+      if (2 * f.tiles * f.parts() * FEW_ROWS * (int)p.tokens * 4 > FEW_TABLE / 2) continue;
+      const int left = FEW_BEFORE - 1024 - f.scale_bytes();   // (shared memory starts at up to 2 KB)
+      if (left >= 0 && left / f.xs + (FEW_AFTER - f.stages * FEW_STAGE) / f.xs >= p.tokens) return true;
+    }
+  return false;
+}
+
+template <class T, int Q, int NT, bool SCALED>
+cudaError_t few_launch(const CodesParams& p, const FewPlan& f, int sms, cudaStream_t st) {
+  static PerDevice limit;
+  const cudaError_t rc = allow_smem(limit, idkm_codes_few<T, Q, NT, SCALED>, FEW_SMEM);
+  if (rc != cudaSuccess) return rc;
+  const long long tiles = (p.rows + FEW_ROWS - 1) / FEW_ROWS;
+  idkm_codes_few<T, Q, NT, SCALED><<<(int)(tiles < sms ? tiles : sms), FEW_BLOCK + 32, FEW_SMEM, st>>>(p, f);
+  return cudaGetLastError();
+}
+
+template <class T, int Q, bool SCALED>
+cudaError_t few_launch(const CodesParams& p, const FewPlan& f, int sms, cudaStream_t st) {
+  return p.tokens <= 8 ? few_launch<T, Q, 1, SCALED>(p, f, sms, st) : few_launch<T, Q, 2, SCALED>(p, f, sms, st);
+}
+
 }  // namespace
 
 extern "C" int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_t ldx, const unsigned char* codes, int64_t rows, int64_t cols,
@@ -109,6 +527,14 @@ extern "C" int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_
   const long long blocks = (rows + ROWS_BLOCK / 32 - 1) / (ROWS_BLOCK / 32);
   return with_type(type, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
+    if constexpr (sizeof(T) == 2) {
+      FewPlan f;
+      if (few_plan(p, f)) {
+        const cudaError_t rc = !scales ? few_launch<T, 1, false>(p, f, sms, st) : p.group == 32 ? few_launch<T, 4, true>(p, f, sms, st)
+                               : p.group == 64 ? few_launch<T, 2, true>(p, f, sms, st) : few_launch<T, 1, true>(p, f, sms, st);
+        return rc == cudaSuccess ? IDKM_OK : IDKM_ERR_CUDA;
+      }
+    }
     constexpr int TOK = 4;
     const long long tiles = (tokens + TOK - 1) / TOK;
     for (long long at = 0; at < tiles; at += 65535) {   // (a grid's second dimension)
