@@ -1,0 +1,72 @@
+// What the kernels of products with 4-bit codes share.
+#pragma once
+#include <cuda_runtime.h>
+#include <stdint.h>
+#include "idkm_types.cuh"
+
+namespace idkm {
+
+struct CodesParams {
+  const void* X;
+  long long tokens, ldx;
+  const unsigned char* codes;
+  long long rows, cols, pitch;
+  const void* C;
+  int k;
+  const void* scales;
+  long long group, n_groups;
+  void* Y;
+  long long ldy;
+  int vec_x;   // rows of X start on 16-byte boundaries
+};
+
+// Products for many rows of 16-bit X, on the tensor cores (idkm_codes_prompt.cu).
+cudaError_t codes_prompt(const CodesParams& p, int type, int sms, cudaStream_t st);
+
+__device__ __forceinline__ float code_scale(unsigned short u, __nv_bfloat16*) { return __uint_as_float((unsigned)u << 16); }
+__device__ __forceinline__ float code_scale(unsigned short u, __half*) { return __half2float(__ushort_as_half(u)); }
+
+// Eight 16-bit elements of a row from column k on, zeros past its end, whatever the row's alignment: from the one or two
+// 16-byte words that hold them.  (A word that holds one byte of the row lies in the row's pages.)
+__device__ __forceinline__ uint4 code_load8(const void* row, long long k, long long cols) {
+  uint4 r = make_uint4(0u, 0u, 0u, 0u);
+  if (k >= cols) return r;
+  const uintptr_t at = (uintptr_t)row + 2 * k, end = (uintptr_t)row + 2 * cols;
+  const uint4* word = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+  const unsigned off = (unsigned)(at & 15u);
+  r = __ldg(word);
+  if (off) {
+    uint4 h = make_uint4(0u, 0u, 0u, 0u);
+    if ((uintptr_t)(word + 1) < end) h = __ldg(word + 1);
+    unsigned w[8] = {r.x, r.y, r.z, r.w, h.x, h.y, h.z, h.w};
+    if (off & 8u) { w[0] = w[2]; w[1] = w[3]; w[2] = w[4]; w[3] = w[5]; w[4] = w[6]; w[5] = w[7]; }
+    if (off & 4u) { w[0] = w[1]; w[1] = w[2]; w[2] = w[3]; w[3] = w[4]; w[4] = w[5]; }
+    if (off & 2u) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+    }
+    r = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  if (k + 8 > cols) {
+    const int keep = (int)(cols - k);   // 1 to 7 elements
+    r.x &= keep >= 2 ? ~0u : 0xffffu;
+    r.y &= keep >= 4 ? ~0u : keep == 3 ? 0xffffu : 0u;
+    r.z &= keep >= 6 ? ~0u : keep == 5 ? 0xffffu : 0u;
+    r.w &= keep == 7 ? 0xffffu : 0u;
+  }
+  return r;
+}
+
+constexpr int CODE_POLLS = 1 << 22;   // (each waits for some time itself)
+__device__ __forceinline__ bool code_wait(unsigned bar, unsigned parity) {
+  for (int i = 0; i < CODE_POLLS; ++i) {
+    unsigned done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (done) return true;
+  }
+  return false;
+}
+__device__ __forceinline__ void code_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+
+}  // namespace idkm

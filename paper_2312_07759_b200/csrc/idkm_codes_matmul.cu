@@ -4,26 +4,12 @@
 #include <stdint.h>
 #include <type_traits>
 #include "idkm_per_device.h"
-#include "idkm_types.cuh"
+#include "idkm_codes.cuh"
 #include "../../include/idkm.h"
 
 namespace {
 
 using namespace idkm;
-
-struct CodesParams {
-  const void* X;
-  long long tokens, ldx;
-  const unsigned char* codes;
-  long long rows, cols, pitch;
-  const void* C;
-  int k;
-  const void* scales;
-  long long group, n_groups;
-  void* Y;
-  long long ldy;
-  int vec_x;   // rows of X start on 16-byte boundaries
-};
 
 constexpr int ROWS_BLOCK = 256;
 constexpr int ROWS_LANE = 8;   // consecutive weights of a lane: one word of codes
@@ -108,7 +94,6 @@ constexpr int FEW_STRIPS = 2, FEW_CHUNK = 128 * FEW_STRIPS;
 constexpr int FEW_PITCH = FEW_WARPS * (FEW_CHUNK / 2) + 64, FEW_STAGE = FEW_ROWS * FEW_PITCH;   // (two rows' 64 bytes in different banks)
 constexpr int FEW_TABLE = 64 * 1024, FEW_SMEM = 227 * 1024 - 256, FEW_TILES = 16;               // tiles of a batch, at most
 constexpr int FEW_BEFORE = FEW_TABLE - 1024, FEW_AFTER = FEW_SMEM - FEW_BEFORE - FEW_TABLE;     // shared memory starts at 1 KB
-constexpr int FEW_POLLS = 1 << 22;   // (each waits for some time itself)
 
 __device__ __forceinline__ void few_mma(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1, __nv_bfloat16*) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -121,40 +106,6 @@ __device__ __forceinline__ void few_mma(float (&c)[4], const unsigned (&a)[4], u
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void few_mma(float (&)[4], const unsigned (&)[4], unsigned, unsigned, float*) {}
-
-__device__ __forceinline__ float few_scale(unsigned short u, __nv_bfloat16*) { return __uint_as_float((unsigned)u << 16); }
-__device__ __forceinline__ float few_scale(unsigned short u, __half*) { return __half2float(__ushort_as_half(u)); }
-
-// Eight 16-bit elements of a row from column k on, zeros past its end, whatever the row's alignment: from the one or two
-// 16-byte words that hold them.  (A word that holds one byte of the row lies in the row's pages.)
-__device__ __forceinline__ uint4 few_load8(const void* row, long long k, long long cols) {
-  uint4 r = make_uint4(0u, 0u, 0u, 0u);
-  if (k >= cols) return r;
-  const uintptr_t at = (uintptr_t)row + 2 * k, end = (uintptr_t)row + 2 * cols;
-  const uint4* word = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
-  const unsigned off = (unsigned)(at & 15u);
-  r = __ldg(word);
-  if (off) {
-    uint4 h = make_uint4(0u, 0u, 0u, 0u);
-    if ((uintptr_t)(word + 1) < end) h = __ldg(word + 1);
-    unsigned w[8] = {r.x, r.y, r.z, r.w, h.x, h.y, h.z, h.w};
-    if (off & 8u) { w[0] = w[2]; w[1] = w[3]; w[2] = w[4]; w[3] = w[5]; w[4] = w[6]; w[5] = w[7]; }
-    if (off & 4u) { w[0] = w[1]; w[1] = w[2]; w[2] = w[3]; w[3] = w[4]; w[4] = w[5]; }
-    if (off & 2u) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
-    }
-    r = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-  if (k + 8 > cols) {
-    const int keep = (int)(cols - k);   // 1 to 7 elements
-    r.x &= keep >= 2 ? ~0u : 0xffffu;
-    r.y &= keep >= 4 ? ~0u : keep == 3 ? 0xffffu : 0u;
-    r.z &= keep >= 6 ? ~0u : keep == 5 ? 0xffffu : 0u;
-    r.w &= keep == 7 ? 0xffffu : 0u;
-  }
-  return r;
-}
 
 // Words w[q] of threads t = 0..3 of a quad: Q = 4: thread t gets word t of thread q's; Q = 2: of the threads with q / 2 = t / 2 words
 // 2 (t % 2) and 2 (t % 2) + 1 -- so that w[q] of the whole quad belongs to group q Q / 4 of the chunk.
@@ -178,19 +129,6 @@ template <int Q>
 __host__ __device__ __forceinline__ constexpr int few_column(int q, int t) {
   // word j of thread s stands for eight 4 s + j
   return Q == 1 ? 4 * t + q : Q == 2 ? 4 * ((q & 2) + (t & 1)) + (t & 2) + (q & 1) : 4 * q + t;
-}
-
-__device__ __forceinline__ bool few_wait(unsigned bar, unsigned parity) {
-  for (int i = 0; i < FEW_POLLS; ++i) {
-    unsigned done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    if (done) return true;
-  }
-  return false;
-}
-__device__ __forceinline__ void few_arrive(unsigned bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 // How a product is taken: tiles of a batch, stages of codes, words of a row's scales in shared memory (odd: a bank a row), bytes of
@@ -244,7 +182,7 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
         int tile = batch, chunk = 0;
         for (int s = 0; s < steps; s += FEW_WARPS) {
           const unsigned bar = full + 8 * stage;
-          if (filled && !few_wait(empty + 8 * stage, (turn & 1) ^ 1)) return;
+          if (filled && !code_wait(empty + 8 * stage, (turn & 1) ^ 1)) return;
           unsigned to = stage0 + stage * FEW_STAGE + lane * FEW_PITCH;
           for (int left = min(FEW_WARPS, steps - s); left > 0;) {
             const int n = min(left, chunks - chunk);
@@ -263,7 +201,7 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
               ++tile;
             }
           }
-          few_arrive(bar);
+          code_arrive(bar);
           if (++stage == f.stages) {
             stage = 0;
             turn ^= 1;
@@ -290,7 +228,7 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
   const int words = chunks * (FEW_CHUNK / 8), n_words = tokens * words;   // 16-byte words of a row of X
   auto place_x = [&](int i, bool load, uint4& x) {
     const int m = i / words, v = i - m * words, place = v & 15;   // place 4 q + t of a strip: for word q of thread t
-    if (load) x = few_load8(reinterpret_cast<const T*>(p.X) + m * p.ldx, (long long)(v >> 4) * 128 + 8 * few_column<Q>(place >> 2, place & 3), p.cols);
+    if (load) x = code_load8(reinterpret_cast<const T*>(p.X) + m * p.ldx, (long long)(v >> 4) * 128 + 8 * few_column<Q>(place >> 2, place & 3), p.cols);
     else *reinterpret_cast<uint4*>(row_of(m) + v * 16) = x;
   };
   {
@@ -348,7 +286,7 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
     const int n_batch = min(f.tiles, tile1 - batch), steps = n_batch * chunks;
     int tile = warp / chunks, chunk = warp % chunks;   // of the batch
     for (int s = 0; s < steps; s += FEW_WARPS) {
-      if (!lost) lost = !few_wait(full + 8 * stage, stage_turn);
+      if (!lost) lost = !code_wait(full + 8 * stage, stage_turn);
       uint4 w[FEW_STRIPS][2];
 #pragma unroll
       for (int u = 0; u < FEW_STRIPS; ++u)
@@ -404,7 +342,7 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
               for (int h = 0; h < 2; ++h) {   // (past the last group only where the codes are past the last column too)
                 unsigned short v = 0;
                 if (g < n_groups) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(scale_of[h] + 2 * g));
-                sc[h] = few_scale(v, type);
+                sc[h] = code_scale(v, type);
               }
 #pragma unroll
               for (int n = 0; n < NT; ++n)
@@ -443,7 +381,7 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
       }
       // (the codes have been used, so they have been read)
       __syncwarp();
-      if (lane == 0) few_arrive(empty + 8 * stage);
+      if (lane == 0) code_arrive(empty + 8 * stage);
       if (++stage == f.stages) {
         stage = 0;
         stage_turn ^= 1;
@@ -534,6 +472,7 @@ extern "C" int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_
                                : p.group == 64 ? few_launch<T, 2, true>(p, f, sms, st) : few_launch<T, 1, true>(p, f, sms, st);
         return rc == cudaSuccess ? IDKM_OK : IDKM_ERR_CUDA;
       }
+      if (tokens > 8) return codes_prompt(p, type, sms, st) == cudaSuccess ? IDKM_OK : IDKM_ERR_CUDA;
     }
     constexpr int TOK = 4;
     const long long tiles = (tokens + TOK - 1) / TOK;
