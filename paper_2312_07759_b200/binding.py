@@ -191,91 +191,103 @@ def assign(W, Cm, want_codes: bool = True, want_Wq: bool = True, stream=None):
 _ELEM = {}   # element types by torch's names for them, as idkm_set_wq_dtype numbers them
 
 
-def _elem(t, *others) -> int:
-    """The number of a tensor's element type; ``others`` have to be of the same."""
-    if not _ELEM:
-        import torch
-        _ELEM.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+def _elem(t) -> int:
+    """The number of a tensor's element type."""
     e = _ELEM.get(t.dtype)
     if e is None:
+        if not _ELEM:
+            import torch
+            _ELEM.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+            return _elem(t)
         raise IdkmError(ERR_UNSUPPORTED)
-    for o in others:
-        if o is not None and o.dtype != t.dtype:
-            raise ValueError(f"tensors of one element type expected: {t.dtype} and {o.dtype}")
     return e
 
 
-def _ld(t) -> int:
-    """Elements between the rows of a matrix whose rows are contiguous."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
-        raise ValueError(f"a matrix with contiguous rows expected, not shape {tuple(t.shape)} with strides {t.stride()}")
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _matrix(t):
+    """(rows, columns, elements between rows) of a matrix whose rows are contiguous."""
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 2 or (stride[1] != 1 and shape[1] > 1):
+        raise ValueError(f"a matrix with contiguous rows expected, not shape {tuple(shape)} with strides {stride}")
+    return shape[0], shape[1], stride[0] if shape[0] > 1 else shape[1]
 
 
 class _Place:
-    """Where a call runs: the device of its first tensor, which all of them have to be on, and the stream -- ``stream``, or that
-    device's current one.  Inside the ``with``, new tensors belong to that stream."""
-    __slots__ = ("handle", "_with", "_dev")
+    """Where a call runs that does not run on the current stream of the current device: inside the ``with`` that device is
+    current, and new tensors belong to that stream."""
+    __slots__ = ("handle", "_with")
 
-    def __init__(self, stream, first, *others):
-        if not first.is_cuda:
-            raise ValueError("tensors on a CUDA device expected")
-        self._dev = dev = first.device
-        for o in others:
-            if o is not None and o.device != dev:
-                raise ValueError(f"tensors on one device expected: {dev} and {o.device}")
+    def __init__(self, stream, dev):
         import torch
-        self._with = None
-        if stream is not None:
-            if not hasattr(stream, "cuda_stream"):
-                stream = torch.cuda.ExternalStream(int(stream), device=dev)
-            if stream.device != dev:
-                raise ValueError(f"a stream of {dev} expected, not of {stream.device}")
-            self._with = torch.cuda.stream(stream)
-            self.handle = int(stream.cuda_stream) or None
-        else:
-            if torch.cuda.current_device() != dev.index:
-                self._with = torch.cuda.device(dev)
-            self.handle = torch._C._cuda_getCurrentRawStream(dev.index) or None
+        if stream is None:
+            self._with = torch.cuda.device(dev)
+            self.handle = torch.cuda.current_stream(dev).cuda_stream or None
+            return
+        if not hasattr(stream, "cuda_stream"):
+            stream = torch.cuda.ExternalStream(int(stream), device=dev)
+        if stream.device.index != dev:
+            raise ValueError(f"a stream of device {dev} expected, not of {stream.device}")
+        self._with = torch.cuda.stream(stream)
+        self.handle = int(stream.cuda_stream) or None
 
     def __enter__(self):
-        if self._with is not None:
-            self._with.__enter__()
+        self._with.__enter__()
         return self
 
     def __exit__(self, *a):
-        if self._with is not None:
-            self._with.__exit__(*a)
+        self._with.__exit__(*a)
+
+
+def _run(stream, call, first, *others):
+    """``call(stream handle)`` on the device of the tensors, which have to be on one, and on ``stream``, or that device's current
+    one.  (A call on the current device's current stream, the usual case, costs no context manager.)"""
+    import torch
+    dev = first.get_device()
+    if dev < 0:
+        raise ValueError("tensors on a CUDA device expected")
+    for o in others:
+        if o is not None and o.get_device() != dev:
+            raise ValueError(f"tensors on one device expected: {first.device} and {o.device}")
+    if stream is None and torch._C._cuda_getDevice() == dev:
+        return call(torch._C._cuda_getCurrentRawStream(dev) or None)
+    with _Place(stream, dev) as at:
+        return call(at.handle)
 
 
 def _apart(out, *inputs) -> None:
     """A given output may not share memory with an input."""
-    lo = out.data_ptr()
-    hi = lo + (sum((n - 1) * st for n, st in zip(out.shape, out.stride())) + 1) * out.element_size()
+    base, span = out.untyped_storage().data_ptr(), None
     for t in inputs:
-        if t is not None and t.numel():
-            a = t.data_ptr()
-            b = a + (sum((n - 1) * st for n, st in zip(t.shape, t.stride())) + 1) * t.element_size()
-            if a < hi and lo < b:
+        if t is not None and t.untyped_storage().data_ptr() == base and t.numel():
+            if span is None:
+                span = _span(out)
+            a, b = _span(t)
+            if a < span[1] and span[0] < b:
                 raise ValueError("the output shares memory with an input")
+
+
+def _span(t):
+    a = t.data_ptr()
+    return a, a + (sum((n - 1) * st for n, st in zip(t.shape, t.stride())) + 1) * t.element_size()
 
 
 def assign_groups(W, Cm, group: int, want_Wq: bool = False, stream=None):
     """``idkm_assign_groups``: 4-bit codes (uint8 [rows, 16 ceil(cols / 32)]), scales ([rows, ceil(cols / group)], of the type of
     the codebook ``Cm``) and, if wanted, the dequantised weights (of W's type) of a CUDA matrix W; ``Cm`` holds k <= 16 entries."""
-    import torch
-    e, ew, ld = _elem(Cm), _elem(W), _ld(W)
-    rows, cols = W.shape
+    e, ew, (rows, cols, ld) = _elem(Cm), _elem(W), _matrix(W)
     if not Cm.is_contiguous() or group < 1:
         raise ValueError("a contiguous codebook and a positive group expected")
-    with _Place(stream, W, Cm) as at:
-        dev = W.device
-        codes = torch.empty((rows, (cols + 31) // 32 * 16), dtype=torch.uint8, device=dev)
-        scales = torch.empty((rows, -(-cols // group)), dtype=Cm.dtype, device=dev)
-        Wq = torch.empty((rows, cols), dtype=W.dtype, device=dev) if want_Wq else None
-        rc = lib.idkm_assign_groups(W.data_ptr(), ew, rows, cols, ld, Cm.data_ptr(), Cm.numel(), e, group, codes.data_ptr(),
-                                    scales.data_ptr(), _ptr(Wq), at.handle)
-    _check(rc)
+
+    def call(handle):
+        import torch
+        codes = torch.empty((rows, (cols + 31) // 32 * 16), dtype=torch.uint8, device=W.device)
+        scales = Cm.new_empty((rows, -(-cols // group)))
+        Wq = W.new_empty((rows, cols)) if want_Wq else None
+        return codes, scales, Wq, lib.idkm_assign_groups(W.data_ptr(), ew, rows, cols, ld, Cm.data_ptr(), Cm.numel(), e, group, codes.data_ptr(),
+                                                         scales.data_ptr(), Wq.data_ptr() if want_Wq else None, handle)
+
+    codes, scales, Wq, rc = _run(stream, call, W, Cm)
+    if rc:
+        raise IdkmError(rc)
     return codes, scales, Wq
 
 
@@ -283,69 +295,82 @@ def matmul_codes(X, codes, Cm, scales=None, group: int = 0, out=None, stream=Non
     """``idkm_matmul_codes``: X [tokens, cols] times the transpose of the weights that ``codes`` ([rows, bytes], uint8, as
     ``assign_groups`` gives them; those of ``assign`` reshaped to rows) stand for with the codebook ``Cm`` and ``scales``
     ([rows, ceil(cols / group)], or None); returns [tokens, rows] of X's type, which is that of the codebook and the scales."""
+    e, (tokens, cols, ldx), (rows, bytes_, pitch) = _elem(X), _matrix(X), _matrix(codes)
+    if Cm.dtype != X.dtype or (scales is not None and scales.dtype != X.dtype):
+        raise ValueError("X, codebook and scales of one element type expected")
     import torch
-    e, ldx = _elem(X, Cm, scales), _ld(X)
-    tokens, cols = X.shape
-    pitch, rows = _ld(codes), codes.shape[0]
-    if codes.dtype != torch.uint8 or 2 * codes.shape[1] < cols or not Cm.is_contiguous():
+    if codes.dtype is not torch.uint8 or 2 * bytes_ < cols or not Cm.is_contiguous():
         raise ValueError("uint8 codes of at least cols / 2 bytes a row and a contiguous codebook expected")
     if scales is not None and (group < 1 or scales.shape != (rows, -(-cols // group)) or not scales.is_contiguous()):
         raise ValueError(f"contiguous scales of shape ({rows}, cols / group) expected")
-    if codes.shape[1] < (cols + 31) // 32 * 16:
+    if bytes_ < (cols + 31) // 32 * 16:
         raise IdkmError(ERR_SHAPE)
-    with _Place(stream, X, codes, Cm, scales) as at:
-        if out is None:
-            out = torch.empty((tokens, rows), dtype=X.dtype, device=X.device)
-            ldy = rows
-        else:
-            if out.shape != (tokens, rows) or out.dtype != X.dtype or out.device != X.device:
-                raise ValueError(f"an output of shape ({tokens}, {rows}) and of X's type and device expected")
-            _apart(out, X, codes, Cm, scales)
-            ldy = _ld(out)
-        rc = lib.idkm_matmul_codes(X.data_ptr(), e, tokens, ldx, codes.data_ptr(), rows, cols, pitch, Cm.data_ptr(), Cm.numel(),
-                                   None if scales is None else scales.data_ptr(), group, out.data_ptr(), ldy, at.handle)
-    _check(rc)
-    return out
+    ldy = rows
+    if out is not None:
+        if out.shape != (tokens, rows) or out.dtype != X.dtype or out.device != X.device:
+            raise ValueError(f"an output of shape ({tokens}, {rows}) and of X's type and device expected")
+        _apart(out, X, codes, Cm, scales)
+        ldy = _matrix(out)[2]
+
+    def call(handle):
+        Y = X.new_empty((tokens, rows)) if out is None else out
+        return Y, lib.idkm_matmul_codes(X.data_ptr(), e, tokens, ldx, codes.data_ptr(), rows, cols, pitch, Cm.data_ptr(), Cm.numel(),
+                                        None if scales is None else scales.data_ptr(), group, Y.data_ptr(), ldy, handle)
+
+    Y, rc = _run(stream, call, X, codes, Cm, scales)
+    if rc:
+        raise IdkmError(rc)
+    return Y
 
 
 def _distill_inputs(z, idx, t, tau):
     import torch
-    if idx.dtype not in (torch.int64, torch.int32):
+    rows, vocab, ld = _matrix(z)
+    shape, size = idx.shape, idx.element_size()
+    if idx.dtype is not torch.int64 and idx.dtype is not torch.int32:
         raise ValueError("indices of 32 or 64 bits expected")
-    if idx.dim() != 2 or idx.shape != t.shape or idx.shape[0] != z.shape[0] or not idx.is_contiguous() or not t.is_contiguous():
+    if len(shape) != 2 or shape != t.shape or shape[0] != rows or not idx.is_contiguous() or not t.is_contiguous():
         raise ValueError("contiguous indices and logits of the teacher of one shape (rows, top) expected")
-    return (z.data_ptr(), _elem(z), z.shape[0], z.shape[1], _ld(z), idx.data_ptr(), 8 if idx.dtype == torch.int64 else 4,
-            t.data_ptr(), _elem(t), idx.shape[1], float(tau))
+    return z.data_ptr(), _elem(z), rows, vocab, ld, idx.data_ptr(), size, t.data_ptr(), _elem(t), shape[1], tau
 
 
-def _row_floats(x, rows, name):
+def _row_weights(weight, rows):
+    """The address of the rows' weights, or None."""
+    if weight is None:
+        return None
     import torch
-    if x is not None and (x.dtype != torch.float32 or x.shape != (rows,) or not x.is_contiguous()):
-        raise ValueError(f"{name}: contiguous float32 of shape ({rows},) expected")
+    if weight.dtype is not torch.float32 or weight.shape != (rows,) or not weight.is_contiguous():
+        raise ValueError(f"weight: contiguous float32 of shape ({rows},) expected")
+    return weight.data_ptr()
 
 
 def _distill_out(z, out, *inputs):
-    import torch
+    """Elements between the rows of the gradient."""
     if out is None:
-        return torch.empty(z.shape, dtype=z.dtype, device=z.device)
+        return z.shape[1]
     if out.shape != z.shape or out.dtype != z.dtype or out.device != z.device:
         raise ValueError("an output of z's shape, type and device expected")
     _apart(out, *inputs)
-    if out.data_ptr() != z.data_ptr() or _ld(out) != _ld(z):
+    ld = _matrix(out)[2]
+    if out.data_ptr() != z.data_ptr() or ld != _matrix(z)[2]:
         _apart(out, z)
-    return out
+    return ld
 
 
 def distill_forward(z, idx, t, tau: float, stream=None):
     """``idkm_distill_forward``: (loss [rows], statistics [rows, 2] for ``distill_backward``), both float32, of the student's logits
     z [rows, vocab] against the teacher's logits t [rows, top] at the indices idx [rows, top] (int32 or int64; -1: no entry)."""
-    import torch
     a = _distill_inputs(z, idx, t, tau)
-    with _Place(stream, z, idx, t) as at:
-        loss = torch.empty(z.shape[0], dtype=torch.float32, device=z.device)
-        stats = torch.empty((z.shape[0], 2), dtype=torch.float32, device=z.device)
-        rc = lib.idkm_distill_forward(*a, loss.data_ptr(), stats.data_ptr(), at.handle)
-    _check(rc)
+
+    def call(handle):
+        import torch
+        loss = torch.empty(a[2], dtype=torch.float32, device=z.device)
+        stats = loss.new_empty((a[2], 2))
+        return loss, stats, lib.idkm_distill_forward(*a, loss.data_ptr(), stats.data_ptr(), handle)
+
+    loss, stats, rc = _run(stream, call, z, idx, t)
+    if rc:
+        raise IdkmError(rc)
     return loss, stats
 
 
@@ -354,28 +379,36 @@ def distill_backward(z, idx, t, tau: float, stats, weight=None, out=None, stream
     [rows], dL/dloss; None: 1), from the statistics of ``distill_forward``.  ``out`` may be z itself."""
     import torch
     a = _distill_inputs(z, idx, t, tau)
-    _row_floats(weight, z.shape[0], "weight")
-    if stats.dtype != torch.float32 or stats.shape != (z.shape[0], 2) or not stats.is_contiguous():
+    w = _row_weights(weight, a[2])
+    if stats.dtype is not torch.float32 or stats.shape != (a[2], 2) or not stats.is_contiguous():
         raise ValueError("the statistics of distill_forward expected")
-    with _Place(stream, z, idx, t, stats, weight) as at:
-        dz = _distill_out(z, out, idx, t, stats, weight)
-        rc = lib.idkm_distill_backward(*a, stats.data_ptr(), None if weight is None else weight.data_ptr(), dz.data_ptr(), _ld(dz),
-                                       at.handle)
-    _check(rc)
+    ld = _distill_out(z, out, idx, t, stats, weight)
+
+    def call(handle):
+        dz = z.new_empty((a[2], a[3])) if out is None else out
+        return dz, lib.idkm_distill_backward(*a, stats.data_ptr(), w, dz.data_ptr(), ld, handle)
+
+    dz, rc = _run(stream, call, z, idx, t, stats, weight, out)
+    if rc:
+        raise IdkmError(rc)
     return dz
 
 
 def distill_step(z, idx, t, tau: float, weight=None, out=None, stream=None):
     """``idkm_distill_step``: (loss [rows], gradient [rows, vocab]) in one launch.  ``out`` may be z itself."""
-    import torch
     a = _distill_inputs(z, idx, t, tau)
-    _row_floats(weight, z.shape[0], "weight")
-    with _Place(stream, z, idx, t, weight) as at:
-        loss = torch.empty(z.shape[0], dtype=torch.float32, device=z.device)
-        dz = _distill_out(z, out, idx, t, weight)
-        rc = lib.idkm_distill_step(*a, None if weight is None else weight.data_ptr(), loss.data_ptr(), dz.data_ptr(), _ld(dz),
-                                   at.handle)
-    _check(rc)
+    w = _row_weights(weight, a[2])
+    ld = _distill_out(z, out, idx, t, weight)
+
+    def call(handle):
+        import torch
+        loss = torch.empty(a[2], dtype=torch.float32, device=z.device)
+        dz = z.new_empty((a[2], a[3])) if out is None else out
+        return loss, dz, lib.idkm_distill_step(*a, w, loss.data_ptr(), dz.data_ptr(), ld, handle)
+
+    loss, dz, rc = _run(stream, call, z, idx, t, weight, out)
+    if rc:
+        raise IdkmError(rc)
     return loss, dz
 
 
