@@ -1,15 +1,23 @@
 // Products with 4-bit weights and group scales for many rows of 16-bit X (a prompt, a large batch), on the tensor cores.
 //
-// A block computes tiles of 128 rows of W by N = 2 HN rows of X, W's codes taken apart on the way: a thread of the looking-up
-// warps has a row of W, turns 128 of its codes into 64 pairs of codebook entries (a table of the 256 pairs with a copy for every
-// lane, as for few rows of X) and stores them into tensor memory, where tcgen05.mma takes its first operand from: codes never
-// become weights in shared memory, whose bandwidth the second operand, X, needs.  The scale of a group multiplies its fp32 sum, in
-// registers: two accumulators of HN columns take turns, and while the tensor cores work on one, the threads that keep the
-// sums (a row of W and HN rows of X each) add the other's, times the row's scale, to theirs.  So every product is that of the
-// codebook's own values, as for few rows; a scale multiplied into the operand would be rounded to 8 bits with it.
+// A pair of blocks (a cluster) computes tiles of 256 rows of W, 128 a block, by N = 2 HN rows of X, of which either block holds
+// half (tcgen05 with cta_group::2: a block's X serves the other's rows of W too, so X comes from L2 and through shared memory once
+// for 256 rows).  W's codes are taken apart on the way: a thread of the looking-up warps has a row of W, turns 128 of its codes into
+// 64 pairs of codebook entries (a table of the 256 pairs with a copy for every lane, as for few rows of X) and stores them into tensor
+// memory, where tcgen05.mma takes its first operand from: codes never become weights in shared memory.  The scale of a group
+// multiplies its fp32 sum, in registers: three accumulators of HN columns take turns (with two, the
+// products wait for the sums), and while the tensor cores work on one, the threads that keep the
+// sums (a row of W and HN / 2 rows of X each) add another's, times the row's scale, to theirs.  So every product
+// is that of the codebook's own values, as for few rows; a scale multiplied into the operand would be rounded to 8 bits with it.
 //
-// Roles (16 warps): 0-7 sums, 8-11 lookups, 12 issues the products, 13 the copies (TMA; X whose rows do not start on 16 bytes is
-// copied by warps 13-15).  Every wait is bounded; if one runs out, the block's results are NaN.
+// Roles (24 warps a block): 0-15 sums, 16-19 lookups, 20 issues the products (the first block's, for both), 21 and 22 the copies
+// (TMA; X whose rows do not start on 16 bytes is copied by warps 21-23).  What the issuing thread waits for -- X, lookups, accumulators
+// that have been added -- is counted in the first block's barriers, by both; what it frees it tells both.  Every wait is
+// bounded; if one runs out, the blocks' results are NaN.
+//
+// What bounds it: the sums, whose loads from tensor memory compete with the products' own accumulators for it (without them 198 us
+// of 237, groups of 128; with groups of 32, four times as many, they take twice the products' time), then the products.
+// Measured, 2048 rows through 8192 x 8192 bf16: 237 us, 1160 TFLOP/s, 0.70 of a plain library product's rate in a burst.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -21,54 +29,104 @@
 namespace idkm {
 namespace {
 
-constexpr int PR_M = 128, PR_BLOCK = 512, PR_K = 128;   // rows of W of a tile, threads, columns of a chunk (one buffer of the first operand)
-constexpr int PR_XS = 4, PR_CS = 2;                     // stages of X (64 columns), of codes (256 columns)
-constexpr int PR_TABLE = 32 * 1024, PR_CODES = PR_M * 128;
+constexpr int PR_M = 128, PR_BLOCK = 768, PR_K = 128;   // rows of W of a tile, threads, columns of a chunk (one buffer of the first operand)
+constexpr int PR_XS = 6, PR_CS = 3, PR_DS = 3;          // stages of X (64 columns), of codes (256 columns), accumulators
+// shared memory: the codes before the table, which lies on a multiple of 64 KB (an address is put together by bytes), X after it
+constexpr int PR_TABLE = 64 * 1024, PR_CODES = PR_M * 128, PR_FRONT = PR_TABLE - 1024;   // (shared memory starts at 1 KB or above)
 
 template <int HN>
 struct PrCfg {
-  static constexpr int N = 2 * HN, X_STAGE = N * 128;
-  static constexpr int OFF_CODES = PR_TABLE, OFF_X = OFF_CODES + PR_CS * PR_CODES, BYTES = OFF_X + PR_XS * X_STAGE;
-  static constexpr int SMEM = BYTES + PR_TABLE;   // (the table lies on a multiple of its size)
-  static constexpr int A0 = N, COLS = N + 128 <= 256 ? 256 : 512;   // columns of tensor memory: accumulators, then two buffers of 64
+  static constexpr int N = 2 * HN, X_HALF = HN / 2 * 128, X_STAGE = 2 * X_HALF;   // a block's rows of X for either accumulator
+  static constexpr int SMEM = PR_FRONT + PR_TABLE + PR_XS * X_STAGE;
+  static_assert(SMEM + 1024 + 256 <= 228 * 1024 && PR_CS * PR_CODES + 8192 <= PR_TABLE, "the X stages after the table, the codes' before");
+  static constexpr int A0 = PR_DS * HN, COLS = A0 + 128 <= 256 ? 256 : 512;   // columns of tensor memory: accumulators, then two buffers of 64
 };
 
 __device__ __forceinline__ unsigned pr_smem(const void* p) { return (unsigned)__cvta_generic_to_shared(p); }
 
-// K-major operand of rows of 128 bytes, swizzled by 128: 8 rows are 1024 bytes.
-__device__ __forceinline__ unsigned long long pr_desc(unsigned addr) {
-  return (unsigned long long)((addr >> 4) & 0x3fffu) | (1ull << 16) | (64ull << 32) | (1ull << 46) | (2ull << 61);
+// A product of 16 columns, both blocks' 128 rows by HN rows of X.  b: 16-byte words to the second operand, K-major rows of 128
+// bytes, swizzled by 128, 8 rows 1024 bytes.
+__device__ __forceinline__ void pr_mma(unsigned d, unsigned a, unsigned b, unsigned idesc, unsigned accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 x;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 x, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], x, %3, p;\n\t}" ::"r"(d),
+      "r"(a), "r"(b), "r"(idesc), "r"(accumulate), "n"((int)(64u | (1u << 14) | (2u << 29)))
+      : "memory");
 }
 
-__device__ __forceinline__ void pr_store32(unsigned addr, const unsigned (&v)[32]) {
+__device__ __forceinline__ void pr_store16(unsigned addr, const unsigned (&v)[16]) {
   asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,"
-      "%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
-      "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
-      "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]),
-      "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr), "r"(v[0]), "r"(v[1]),
+      "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]),
+      "r"(v[14]), "r"(v[15])
       : "memory");
 }
-__device__ __forceinline__ void pr_load16(unsigned addr, unsigned (&r)[16]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-        "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(addr)
-      : "memory");
+template <int W>
+__device__ __forceinline__ void pr_load(unsigned addr, unsigned (&r)[W]) {
+  if constexpr (W == 16)
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
+        : "memory");
+  else if constexpr (W == 8)
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(addr)
+                 : "memory");
+  else
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,"
+        "%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+          "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
+          "=r"(r[31])
+        : "r"(addr)
+        : "memory");
 }
 // what has been asked for has arrived; r depends on it
-__device__ __forceinline__ void pr_arrived(unsigned (&r)[16]) {
+template <int W>
+__device__ __forceinline__ void pr_arrived(unsigned (&r)[W]) {
   asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
-  for (int i = 0; i < 16; ++i) asm volatile("" : "+r"(r[i]));
+  for (int i = 0; i < W; ++i) asm volatile("" : "+r"(r[i]));
 }
+// to the barrier of either block, once the products issued so far are done
 __device__ __forceinline__ void pr_commit(unsigned bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((unsigned short)3) : "memory");
 }
 __device__ __forceinline__ void pr_tma(unsigned to, const CUtensorMap* map, int x, int y, unsigned bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+// the same, telling the first block's barrier
+__device__ __forceinline__ void pr_tma_pair(unsigned to, const CUtensorMap* map, int x, int y, unsigned first_bar) {
+  asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+               ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(first_bar) : "memory");
+}
+// the first block's barrier
+__device__ __forceinline__ unsigned pr_first(unsigned bar) {
+  unsigned r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(bar));
+  return r;
+}
+// (What is handed over lies in tensor memory, and the fence before orders it: nothing written to memory has to be waited for.)
+__device__ __forceinline__ void pr_arrive_first(unsigned first_bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(first_bar) : "memory");
+}
+__device__ __forceinline__ void pr_arrive_first_written(unsigned first_bar) {   // ... where it does
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(first_bar) : "memory");
+}
+__device__ __forceinline__ bool pr_wait_both(unsigned bar, unsigned parity) {   // for what both blocks count
+  for (int i = 0; i < CODE_POLLS; ++i) {
+    unsigned done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (done) return true;
+  }
+  return false;
 }
 __device__ __forceinline__ void pr_expect(unsigned bar, int bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -95,17 +153,19 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
   constexpr int STEPS = 8 / SEGS;   // products of 16 columns of a segment
   T* const type = nullptr;
   extern __shared__ __align__(16) unsigned char pr_raw[];
-  __shared__ __align__(8) unsigned long long s_bar[2 * PR_XS + 2 * PR_CS + 8];
+  __shared__ __align__(8) unsigned long long s_bar[2 * PR_XS + 2 * PR_CS + 4 + 2 * PR_DS];
   __shared__ unsigned s_tmem;
   const unsigned raw = pr_smem(pr_raw), base = (raw + PR_TABLE - 1) & ~(unsigned)(PR_TABLE - 1);
-  unsigned char* const mem = pr_raw + (base - raw);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // (codes and X on multiples of 1024, which the swizzle goes by)
+  const unsigned codes0 = base - PR_CS * PR_CODES, x0_at = base + PR_TABLE;
+  unsigned char* const mem_x = pr_raw + (x0_at - raw);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x & 1;
   const unsigned bars = pr_smem(s_bar);
   const unsigned x_full = bars, x_empty = x_full + 8 * PR_XS, c_full = x_empty + 8 * PR_XS, c_empty = c_full + 8 * PR_CS;
-  const unsigned a_full = c_empty + 8 * PR_CS, a_empty = a_full + 16, d_full = a_empty + 16, d_empty = d_full + 16;
+  const unsigned a_full = c_empty + 8 * PR_CS, a_empty = a_full + 16, d_full = a_empty + 16, d_empty = d_full + 8 * PR_DS;
   if (tid == 0) {
     for (int i = 0; i < PR_XS; ++i) {
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(x_full + 8 * i), "r"(TMA ? 1 : 96) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(x_full + 8 * i), "r"(TMA ? 1 : 6) : "memory");
       asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(x_empty + 8 * i) : "memory");
     }
     for (int i = 0; i < PR_CS; ++i) {
@@ -113,45 +173,54 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
       asm volatile("mbarrier.init.shared::cta.b64 [%0], 4;" ::"r"(c_empty + 8 * i) : "memory");
     }
     for (int i = 0; i < 2; ++i) {
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 4;" ::"r"(a_full + 8 * i) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 8;" ::"r"(a_full + 8 * i) : "memory");
       asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(a_empty + 8 * i) : "memory");
+    }
+    for (int i = 0; i < PR_DS; ++i) {
       asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(d_full + 8 * i) : "memory");
-      asm volatile("mbarrier.init.shared::cta.b64 [%0], 4;" ::"r"(d_empty + 8 * i) : "memory");
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], 16;" ::"r"(d_empty + 8 * i) : "memory");
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 12) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(pr_smem(&s_tmem)), "r"(Cfg::COLS) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  if (warp == 20) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(pr_smem(&s_tmem)), "r"(Cfg::COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   if (tid < 256) {   // the pairs of codebook entries, one for every lane
     const unsigned short* c = reinterpret_cast<const unsigned short*>(p.C);
     const unsigned lo = (tid & 15) < p.k ? __ldg(c + (tid & 15)) : 0u, hi = (tid >> 4) < p.k ? __ldg(c + (tid >> 4)) : 0u, both = lo | hi << 16;
 #pragma unroll
     for (int q = 0; q < 8; ++q)
-      asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(base + tid * 128 + ((q + lane) & 7) * 16), "r"(both) : "memory");
+      asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(base + tid * 256 + ((q + lane) & 7) * 16), "r"(both) : "memory");
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  // (both blocks run, their barriers are ready)
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const unsigned tmem = *reinterpret_cast<volatile unsigned*>(&s_tmem);
 
   const int n_chunks = (int)((p.cols + PR_K - 1) / PR_K);
-  const long long tiles_x = (p.tokens + Cfg::N - 1) / Cfg::N, tiles = tiles_x * ((p.rows + PR_M - 1) / PR_M);
+  const long long tiles_x = (p.tokens + Cfg::N - 1) / Cfg::N, tiles = tiles_x * ((p.rows + 2 * PR_M - 1) / (2 * PR_M));
+  const long long tile0 = blockIdx.x >> 1, tile_on = gridDim.x >> 1;
   bool ok = true;
 
-  if (warp < 8) {   // ---- the sums
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
-    const int h = warp >> 2, quad = warp & 3;
-    const unsigned from = tmem + ((unsigned)(quad * 32) << 16) + (unsigned)(h * HN);
+  if (warp < 16) {   // ---- the sums
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 96;");
+    constexpr int HC = HN / 2;   // columns of a thread
+    const int h = warp >> 3, part = warp >> 2 & 1, quad = warp & 3;
+    const unsigned from0 = tmem + ((unsigned)(quad * 32) << 16) + (unsigned)(part * HC);
     const int per = SEGS > 1 ? 1 : (int)(p.group / PR_K);   // chunks of a group
+    const unsigned d_added = pr_first(d_empty);
+    int buffer = h;        // every second accumulation is this half's, the accumulators take turns
     unsigned parity = 0;
-    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-      const long long row = tile / tiles_x * PR_M + quad * 32 + lane, tok0 = tile % tiles_x * Cfg::N + h * HN;
+    for (long long tile = tile0; tile < tiles; tile += tile_on) {
+      const long long row = (tile / tiles_x * 2 + rank) * PR_M + quad * 32 + lane, tok0 = tile % tiles_x * Cfg::N + h * HN + part * HC;
       const unsigned short* s_row = p.scales && row < p.rows ? reinterpret_cast<const unsigned short*>(p.scales) + row * p.n_groups : nullptr;
-      float acc[HN];
+      float acc[HC];
 #pragma unroll
-      for (int i = 0; i < HN; ++i) acc[i] = 0.f;
+      for (int i = 0; i < HC; ++i) acc[i] = 0.f;
       int g = 0, left = per;   // the group, and chunks of it that are left
       unsigned short next = s_row ? __ldg(s_row) : (unsigned short)0;
 #pragma unroll 1
@@ -163,85 +232,82 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
           next = 0;   // (groups past the last one: columns past the last one, 0)
           if (s_row && g < p.n_groups) next = __ldg(s_row + g);
         }
-        if (ok) ok = code_wait(d_full + 8 * h, parity);
-        parity ^= 1u;
+        if (ok) ok = code_wait(d_full + 8 * buffer, parity);
+        const unsigned from = from0 + (unsigned)(buffer * HN), added = d_added + 8 * buffer;
+        buffer += 2;
+        if (buffer >= PR_DS) {
+          buffer -= PR_DS;
+          parity ^= 1u;
+        }
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        unsigned r0[16], r1[16];
-        auto add = [&](const unsigned (&r)[16], int at) {
+        constexpr int W = HC < 16 ? 8 : 16;
+        unsigned r0[W], r1[W];
+        auto add = [&](const unsigned (&r)[W], int at) {
 #pragma unroll
-          for (int i = 0; i < 16; i += 2)
+          for (int i = 0; i < W; i += 2)
             asm("{\n\t.reg .b64 a, b, c;\n\tmov.b64 a, {%2, %3};\n\tmov.b64 b, {%4, %4};\n\tmov.b64 c, {%0, %1};\n\tfma.rn.f32x2 c, a, b, c;\n\tmov.b64 {%0, %1}, c;\n\t}"
                 : "+f"(acc[at + i]), "+f"(acc[at + i + 1]) : "r"(r[i]), "r"(r[i + 1]), "f"(s));
         };
-        pr_load16(from, r0);
+        auto taken = [&] {   // everything has arrived: the accumulator is free
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) pr_arrive_first(added);
+        };
 #pragma unroll
-        for (int at = 0; at < HN; at += 32) {
+        for (int at = 0; at < HC; at += 2 * W) {
+          pr_load(from + at, r0);
+          if (at + W < HC) pr_load(from + at + W, r1);
           pr_arrived(r0);
-          if (at + 16 < HN) pr_load16(from + at + 16, r1);
-          else {
-            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) code_arrive(d_empty + 8 * h);
-          }
+          if (at + W < HC) pr_arrived(r1);
+          if (at + 2 * W >= HC) taken();
           add(r0, at);
-          if (at + 16 < HN) {
-            pr_arrived(r1);
-            if (at + 32 < HN) pr_load16(from + at + 32, r0);
-            else {
-              asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-              __syncwarp();
-              if (lane == 0) code_arrive(d_empty + 8 * h);
-            }
-            add(r1, at + 16);
-          }
+          if (at + W < HC) add(r1, at + W);
         }
       }
       if (row < p.rows) {
         T* y = reinterpret_cast<T*>(p.Y) + row;
 #pragma unroll
-        for (int i = 0; i < HN; ++i)
+        for (int i = 0; i < HC; ++i)
           if (tok0 + i < p.tokens) y[(tok0 + i) * p.ldy] = from_f32<T>(ok ? acc[i] : __int_as_float(0x7fc00000));
       }
     }
-  } else if (warp < 12) {   // ---- the lookups
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+  } else if (warp < 20) {   // ---- the lookups
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     const int quad = warp & 3, r = quad * 32 + lane;
     unsigned mine;   // (there after the barrier only)
     asm volatile("or.b32 %0, %1, %2;" : "=r"(mine) : "r"(base), "r"((unsigned)lane * 4u) : "memory");
-    const unsigned my_codes = base + Cfg::OFF_CODES + (unsigned)r * 128u;
+    const unsigned my_codes = codes0 + (unsigned)r * 128u;
     const unsigned to = tmem + ((unsigned)(quad * 32) << 16) + (unsigned)Cfg::A0;
+    const unsigned a_there = pr_first(a_full);
     PrRing<PR_CS> cr;
     PrRing<2> ar;
-    for (long long tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+    for (long long tile = tile0; tile < tiles; tile += tile_on) {
 #pragma unroll 1
       for (int c = 0; c < n_chunks; ++c) {
         if (ok && (c & 1) == 0) ok = code_wait(c_full + 8 * cr.at, cr.parity);
+        unsigned w[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[j][0]), "=r"(w[j][1]), "=r"(w[j][2]), "=r"(w[j][3])
+                       : "r"(my_codes + cr.at * PR_CODES + ((((unsigned)(c & 1) * 4u + (unsigned)j) ^ (unsigned)(r & 7)) << 4)) : "memory");
         if (ok) ok = code_wait(a_empty + 8 * ar.at, ar.parity ^ 1u);
         ok = __all_sync(0xffffffffu, ok);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          unsigned v[32];
+        for (int j = 0; j < 4; ++j) {
+          unsigned v[16];
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const unsigned piece = (unsigned)((c & 1) * 4 + half * 2 + j);
-            unsigned w[4];
-            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                         : "r"(my_codes + cr.at * PR_CODES + ((piece ^ (unsigned)(r & 7)) << 4)) : "memory");
+          for (int q = 0; q < 4; ++q)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const unsigned o[4] = {w[q] << 7, w[q] >> 1, w[q] >> 9, w[q] >> 17};
-#pragma unroll
-              for (int i = 0; i < 4; ++i) asm("ld.shared.u32 %0, [%1];" : "=r"(v[j * 16 + q * 4 + i]) : "r"((o[i] & 0x7f80u) | mine));
-            }
-          }
-          pr_store32(to + (unsigned)(ar.at * 64 + half * 32), v);
+            for (int i = 0; i < 4; ++i)   // (the lane's byte, byte i of the codes, the table's two)
+              asm("ld.shared.u32 %0, [%1];" : "=r"(v[q * 4 + i]) : "r"(__byte_perm(mine, w[j][q], 0x3240u + 0x10u * (unsigned)i)));
+          pr_store16(to + (unsigned)(ar.at * 64 + j * 16), v);
         }
         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
         if (lane == 0) {
-          code_arrive(a_full + 8 * ar.at);
+          pr_arrive_first(a_there + 8 * ar.at);
           if ((c & 1) || c + 1 == n_chunks) code_arrive(c_empty + 8 * cr.at);
         }
         if ((c & 1) || c + 1 == n_chunks) cr.next();
@@ -249,90 +315,103 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
       }
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == 12) {   // ---- the products
-      if (lane == 0) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp == 20) {   // ---- the products
+      if (rank == 0) {
+        // The whole warp goes round, so that what the products are given is known to be the same for all lanes; one lane issues.
+        // (One lane going round alone issued a product every 105 cycles, 64 are enough.)
+        unsigned chosen;
+        asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(chosen));
         const unsigned kind = std::is_same<T, __half>::value ? 0u : 1u;
-        const unsigned idesc = (1u << 4) | (kind << 7) | (kind << 10) | ((unsigned)(HN >> 3) << 17) | ((unsigned)(PR_M >> 4) << 24);
+        const unsigned idesc = (1u << 4) | (kind << 7) | (kind << 10) | ((unsigned)(HN >> 3) << 17) | ((unsigned)(2 * PR_M >> 4) << 24);
+        const unsigned d0 = __shfl_sync(0xffffffffu, tmem, 0), x_base = (x0_at >> 4) | (1u << 16);
         PrRing<PR_XS> xr;
         PrRing<2> ar;
-        unsigned d_turn = 1;   // (both accumulators are free at first)
-        for (long long tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
+        PrRing<PR_DS> dr;
+        for (long long tile = tile0; tile < tiles && ok; tile += tile_on) {
 #pragma unroll 1
           for (int c = 0; c < n_chunks && ok; ++c) {
-            ok = code_wait(a_full + 8 * ar.at, ar.parity);
+            ok = pr_wait_both(a_full + 8 * ar.at, ar.parity);
             const int x0 = xr.at;
-            ok = ok && code_wait(x_full + 8 * xr.at, xr.parity);
+            ok = ok && pr_wait_both(x_full + 8 * xr.at, xr.parity);
             xr.next();
             const int x1 = xr.at;
-            ok = ok && code_wait(x_full + 8 * xr.at, xr.parity);
+            ok = ok && pr_wait_both(x_full + 8 * xr.at, xr.parity);
             xr.next();
+            const unsigned b0 = x_base + (unsigned)x0 * (Cfg::X_STAGE / 16), b1 = x_base + (unsigned)x1 * (Cfg::X_STAGE / 16), a0 = d0 + (unsigned)(Cfg::A0 + ar.at * 64);
 #pragma unroll
             for (int seg = 0; seg < SEGS; ++seg) {
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                ok = ok && code_wait(d_empty + 8 * h, d_turn);
+                ok = ok && pr_wait_both(d_empty + 8 * dr.at, dr.parity ^ 1u);
+                ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                if (chosen) {
 #pragma unroll
-                for (int i = 0; i < STEPS; ++i) {
-                  const int k16 = seg * STEPS + i;
-                  const unsigned long long b = pr_desc(base + Cfg::OFF_X + (k16 < 4 ? x0 : x1) * Cfg::X_STAGE + h * HN * 128 + (k16 & 3) * 32);
-                  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                               ::"r"(tmem + (unsigned)(h * HN)), "r"(tmem + (unsigned)(Cfg::A0 + ar.at * 64 + k16 * 8)), "l"(b), "r"(idesc), "r"(i > 0 ? 1u : 0u)
-                               : "memory");
+                  for (int i = 0; i < STEPS; ++i) {
+                    const int k16 = seg * STEPS + i;
+                    pr_mma(d0 + (unsigned)(dr.at * HN), a0 + (unsigned)(k16 * 8), (k16 < 4 ? b0 : b1) + (unsigned)(h * (Cfg::X_HALF / 16) + (k16 & 3) * 2), idesc, i > 0);
+                  }
+                  pr_commit(d_full + 8 * dr.at);
+                  if (seg + 1 == SEGS && h == 1) {
+                    pr_commit(a_empty + 8 * ar.at);
+                    pr_commit(x_empty + 8 * x0);
+                    pr_commit(x_empty + 8 * x1);
+                  }
                 }
-                pr_commit(d_full + 8 * h);
+                __syncwarp();
+                dr.next();
               }
-              d_turn ^= 1u;
-            }
-            if (ok) {
-              pr_commit(a_empty + 8 * ar.at);
-              pr_commit(x_empty + 8 * x0);
-              pr_commit(x_empty + 8 * x1);
             }
             ar.next();
           }
         }
       }
-    } else {   // ---- the copies
+    } else if (!TMA || warp == 21 || warp == 22) {   // ---- the copies: with TMA X by one thread, the codes, which are further ahead, by another
       PrRing<PR_XS> xr;
       PrRing<PR_CS> cr;
       bool x_filled = false, c_filled = false;   // every stage has been filled once
-      for (long long tile = blockIdx.x; tile < tiles && ok; tile += gridDim.x) {
-        const long long row0 = tile / tiles_x * PR_M, tok0 = tile % tiles_x * Cfg::N;
+      const unsigned x_there = pr_first(x_full);
+      for (long long tile = tile0; tile < tiles && ok; tile += tile_on) {
+        const long long row0 = (tile / tiles_x * 2 + rank) * PR_M, tok0 = tile % tiles_x * Cfg::N;
 #pragma unroll 1
         for (int c = 0; c < n_chunks && ok; ++c) {
-          if (warp == 13 && lane == 0 && (c & 1) == 0) {
+          if (warp == (TMA ? 22 : 21) && lane == 0 && (c & 1) == 0) {
             if (c_filled) ok = code_wait(c_empty + 8 * cr.at, cr.parity ^ 1u);
             if (ok) {
               pr_expect(c_full + 8 * cr.at, PR_CODES);
-              pr_tma(base + Cfg::OFF_CODES + cr.at * PR_CODES, &map_codes, c * (PR_K / 2), (int)row0, c_full + 8 * cr.at);
+              pr_tma(codes0 + cr.at * PR_CODES, &map_codes, c * (PR_K / 2), (int)row0, c_full + 8 * cr.at);
               cr.next();
               if (cr.at == 0) c_filled = true;
             }
           }
 #pragma unroll
           for (int j = 0; j < 2; ++j) {
-            const unsigned at = base + Cfg::OFF_X + xr.at * Cfg::X_STAGE;
+            const unsigned at = x0_at + xr.at * Cfg::X_STAGE;
             if (TMA) {
-              if (warp == 13 && lane == 0) {
+              if (warp == 21 && lane == 0) {
                 if (x_filled && ok) ok = code_wait(x_empty + 8 * xr.at, xr.parity ^ 1u);
                 if (ok) {
-                  pr_expect(x_full + 8 * xr.at, Cfg::X_STAGE);
-                  pr_tma(at, &map_x, c * PR_K + j * 64, (int)tok0, x_full + 8 * xr.at);
+                  if (rank == 0) pr_expect(x_full + 8 * xr.at, 2 * Cfg::X_STAGE);   // (of both blocks)
+#pragma unroll
+                  for (int h = 0; h < 2; ++h)
+                    pr_tma_pair(at + h * Cfg::X_HALF, &map_x, c * PR_K + j * 64, (int)tok0 + h * HN + rank * (HN / 2), x_there + 8 * xr.at);
                 }
               }
             } else {
               if (x_filled && ok) ok = code_wait(x_empty + 8 * xr.at, xr.parity ^ 1u);
-              for (int i = tid - 13 * 32; i < Cfg::N * 8; i += 96) {
-                const int m = i >> 3, v = i & 7;
+              ok = __all_sync(0xffffffffu, ok);   // (warps stay together whatever comes of it)
+              for (int i = tid - 21 * 32; i < HN * 8; i += 96) {
+                const int m = i >> 3, v = i & 7, h = m >= HN / 2;   // (halves are whole groups of 8 rows: the swizzle is that of the row in either)
+                const long long tok = tok0 + h * HN + rank * (HN / 2) + (m - h * (HN / 2));
                 uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                if (tok0 + m < p.tokens) x = code_load8(reinterpret_cast<const T*>(p.X) + (tok0 + m) * p.ldx, c * PR_K + j * 64 + v * 8, p.cols);
-                *reinterpret_cast<uint4*>(mem + Cfg::OFF_X + xr.at * Cfg::X_STAGE + m * 128 + ((v ^ (m & 7)) << 4)) = x;
+                if (tok < p.tokens) x = code_load8(reinterpret_cast<const T*>(p.X) + tok * p.ldx, c * PR_K + j * 64 + v * 8, p.cols);
+                *reinterpret_cast<uint4*>(mem_x + xr.at * Cfg::X_STAGE + m * 128 + ((v ^ (m & 7)) << 4)) = x;
               }
               asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-              code_arrive(x_full + 8 * xr.at);
+              __syncwarp();
+              if (lane == 0) pr_arrive_first_written(x_there + 8 * xr.at);
             }
             xr.next();
             if (xr.at == 0) x_filled = true;
@@ -341,17 +420,20 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
       }
       // nothing is left under way when the block ends: every stage that was filled has been waited for by those who read it, unless
       // they gave up
-      if (warp == 13 && lane == 0 && !ok) {
+      if (lane == 0 && !ok) {
         for (int i = 0; i < 2 * PR_CS; ++i) code_wait(c_full + 8 * (i % PR_CS), (unsigned)(i / PR_CS));
-        for (int i = 0; i < 2 * PR_XS; ++i) code_wait(x_full + 8 * (i % PR_XS), (unsigned)(i / PR_XS));
+        for (int i = 0; i < 2 * PR_XS; ++i) code_wait((rank == 0 ? x_full : x_empty) + 8 * (i % PR_XS), (unsigned)(i / PR_XS));
       }
     }
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  // (neither block leaves while the other may still tell it something)
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-  if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Cfg::COLS));
+  if (warp == 20) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Cfg::COLS));
 }
 
 typedef CUresult (*PrEncode)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -381,14 +463,24 @@ cudaError_t pr_launch(const CodesParams& p, int sms, cudaStream_t st) {
   CUtensorMap codes, x = {};
   if (!pr_map(codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.codes, (p.cols + 31) / 32 * 16, p.rows, p.pitch, PR_M)) return cudaErrorInvalidValue;
   if (TMA && !pr_map(x, std::is_same<T, __half>::value ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, p.X, p.cols, p.tokens,
-                     p.ldx * 2, Cfg::N))
+                     p.ldx * 2, HN / 2))
     return cudaErrorInvalidValue;
   static PerDevice limit;
   const cudaError_t rc = allow_smem(limit, idkm_codes_prompt<T, HN, SEGS, TMA>, Cfg::SMEM);
   if (rc != cudaSuccess) return rc;
-  const long long tiles = (p.rows + PR_M - 1) / PR_M * ((p.tokens + Cfg::N - 1) / Cfg::N);
-  idkm_codes_prompt<T, HN, SEGS, TMA><<<(int)(tiles < sms ? tiles : sms), PR_BLOCK, Cfg::SMEM, st>>>(p, codes, x);
-  return cudaGetLastError();
+  const long long tiles = (p.rows + 2 * PR_M - 1) / (2 * PR_M) * ((p.tokens + Cfg::N - 1) / Cfg::N), pairs = sms / 2;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs)));
+  cfg.blockDim = dim3(PR_BLOCK);
+  cfg.dynamicSmemBytes = Cfg::SMEM;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 2;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, idkm_codes_prompt<T, HN, SEGS, TMA>, p, codes, x);
 }
 
 template <class T, int HN>
@@ -403,13 +495,13 @@ cudaError_t pr_launch(const CodesParams& p, int sms, cudaStream_t st) {
 cudaError_t codes_prompt(const CodesParams& p, int type, int sms, cudaStream_t st) {
   if (!pr_encode()) return cudaErrorNotSupported;
   if (p.rows > INT32_MAX - PR_M || p.cols > INT32_MAX - 512 || p.tokens > INT32_MAX - 256) return cudaErrorInvalidValue;
-  // rows of X of a tile: those whose waves of tiles cost least; a chunk costs its products, 4 cycles a row of X, but at least the
-  // lookups (420)
-  const long long tiles_w = (p.rows + PR_M - 1) / PR_M;
+  // rows of X of a tile: those whose waves of tiles cost least.  A chunk of 128 columns took 0.63, 0.66, 0.76 and 0.92 us at HN =
+  // 16, 32, 64 and 128 (2048 rows through 8192 x 8192: 1120, 594, 342 and 237 us in all), about 1200 + 5 HN halves of a nanosecond.
+  const long long tiles_w = (p.rows + 2 * PR_M - 1) / (2 * PR_M), pairs = sms / 2;
   int best = 128;
   long long least = INT64_MAX;
   for (int hn = 16; hn <= 128; hn *= 2) {
-    const long long tiles = tiles_w * ((p.tokens + 2 * hn - 1) / (2 * hn)), cost = (tiles + sms - 1) / sms * (8 * hn > 420 ? 8 * hn : 420);
+    const long long tiles = tiles_w * ((p.tokens + 2 * hn - 1) / (2 * hn)), cost = (tiles + pairs - 1) / pairs * (1200 + 5 * hn);
     if (cost < least || (cost == least && hn <= best)) {
       least = cost;
       best = hn;
