@@ -11,61 +11,115 @@ namespace {
 
 using namespace idkm;
 
-constexpr int ROWS_BLOCK = 256;
+constexpr int ROWS_BLOCK = 256, ROWS_WARPS = ROWS_BLOCK / 32;
 constexpr int ROWS_LANE = 8;   // consecutive weights of a lane: one word of codes
+constexpr int ROWS_OF = 4;     // rows of W of a warp
 
-// A warp takes a row of W and TOK rows of X; every lane looks its eight weights up and adds their products, the group's scale
-// multiplies the sum of the eight.
+// Full precision (and shapes that the kernels below do not take).  A warp takes four rows of W and TOK rows of X, so that what it loads of
+// X serves four rows; every lane looks eight weights of each row up and adds their products, the group's scale multiplies the
+// sum of the eight.  `split` warps of a block share the columns of the same rows, where there are few rows; their sums meet in shared
+// memory in the order of the warps.
+// What bounds it: the multiply-adds and lookups, at 4096 x 4608 fp32 and 5 rows of X 5 and 1 an eight weights.
 template <class T, int TOK>
-__global__ void __launch_bounds__(ROWS_BLOCK) idkm_codes_rows(const CodesParams p) {
+__global__ void __launch_bounds__(ROWS_BLOCK) idkm_codes_rows(const __grid_constant__ CodesParams p, int split) {
   __shared__ float lut[16];
+  __shared__ float part[ROWS_WARPS][ROWS_OF * TOK];
   if (threadIdx.x < 16) lut[threadIdx.x] = threadIdx.x < p.k ? to_f32(reinterpret_cast<const T*>(p.C)[threadIdx.x]) : 0.f;
   __syncthreads();
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = warp % split, sets = ROWS_WARPS / split;
   const long long m0 = (long long)blockIdx.y * TOK;
   const T* X = reinterpret_cast<const T*>(p.X) + m0 * p.ldx;
   const int n_tok = (int)min((long long)TOK, p.tokens - m0);
-  for (long long n = (long long)blockIdx.x * (ROWS_BLOCK / 32) + (threadIdx.x >> 5); n < p.rows; n += (long long)gridDim.x * (ROWS_BLOCK / 32)) {
-    const unsigned char* row = p.codes + n * p.pitch;
-    float acc[TOK];
+  const long long quads = (p.rows + ROWS_OF - 1) / ROWS_OF;
+  for (long long first = (long long)blockIdx.x * sets; first < quads; first += (long long)gridDim.x * sets) {
+    const long long n0 = (first + warp / split) * ROWS_OF;
+    float acc[ROWS_OF][TOK];
 #pragma unroll
-    for (int m = 0; m < TOK; ++m) acc[m] = 0.f;
-    for (long long c = lane * ROWS_LANE; c < p.cols; c += 32 * ROWS_LANE) {
-      const unsigned word = __ldg(reinterpret_cast<const unsigned*>(row + c / 2));
-      const float s = p.scales ? to_f32(reinterpret_cast<const T*>(p.scales)[n * p.n_groups + c / p.group]) : 1.f;
-      float w[ROWS_LANE];
+    for (int r = 0; r < ROWS_OF; ++r)
 #pragma unroll
-      for (int e = 0; e < ROWS_LANE; ++e) w[e] = lut[word >> (4 * e) & 15u];
+      for (int m = 0; m < TOK; ++m) acc[r][m] = 0.f;
+    if (n0 < p.rows) {
+      const int rows = (int)min((long long)ROWS_OF, p.rows - n0);
+      const unsigned char* codes = p.codes + n0 * p.pitch;
+      const T* scales = p.scales ? reinterpret_cast<const T*>(p.scales) + n0 * p.n_groups : nullptr;
+      const long long on = (long long)split * 32 * ROWS_LANE;
+      unsigned word[ROWS_OF], next[ROWS_OF];
+      const unsigned char* row_at[ROWS_OF];
 #pragma unroll
-      for (int m = 0; m < TOK; ++m) {
-        if (m >= n_tok) continue;
-        const T* x = X + m * p.ldx + c;
-        float xs[ROWS_LANE];
-        if (p.vec_x && c + ROWS_LANE <= p.cols) {
+      for (int r = 0; r < ROWS_OF; ++r) row_at[r] = codes + (r < rows ? r : 0) * p.pitch;
+      auto fetch = [&](unsigned (&to)[ROWS_OF], long long c) {   // (rows past the last one: the first's)
+#pragma unroll
+        for (int r = 0; r < ROWS_OF; ++r) {
+          to[r] = 0u;
+          if (c < p.cols) to[r] = __ldg(reinterpret_cast<const unsigned*>(row_at[r] + c / 2));
+        }
+      };
+      long long c = (long long)(mine * 32 + lane) * ROWS_LANE;
+      fetch(word, c);
+      for (; c < p.cols; c += on) {
+        fetch(next, c + on);
+        const bool whole = p.vec_x && c + ROWS_LANE <= p.cols;
+        // X is asked for before anything is looked at; rows past the last one count for nothing
+        float xs[TOK][ROWS_LANE];
+        if (whole) {
           constexpr int N = Vec16<T>::N;
+          Vec16<T> v[TOK][ROWS_LANE / N];
+          const T* x = X + c;
 #pragma unroll
-          for (int q = 0; q < ROWS_LANE / N; ++q) {
-            Vec16<T> v;
-            v.raw = __ldg(reinterpret_cast<const uint4*>(x) + q);
+          for (int m = 0; m < TOK; ++m) {
 #pragma unroll
-            for (int e = 0; e < N; ++e) xs[q * N + e] = to_f32(v.e[e]);
+            for (int q = 0; q < ROWS_LANE / N; ++q) v[m][q].raw = __ldg(reinterpret_cast<const uint4*>(x) + q);
+            if (m + 1 < n_tok) x += p.ldx;   // (rows past the last one: the last)
           }
+#pragma unroll
+          for (int m = 0; m < TOK; ++m)
+#pragma unroll
+            for (int q = 0; q < ROWS_LANE / N; ++q)
+#pragma unroll
+              for (int e = 0; e < N; ++e) xs[m][q * N + e] = to_f32(v[m][q].e[e]);
         } else {
 #pragma unroll
-          for (int e = 0; e < ROWS_LANE; ++e) xs[e] = c + e < p.cols ? to_f32(x[e]) : 0.f;
-        }
-        float sum = 0.f;
+          for (int m = 0; m < TOK; ++m)
 #pragma unroll
-        for (int e = 0; e < ROWS_LANE; ++e) sum = fmaf(w[e], xs[e], sum);
-        acc[m] = fmaf(s, sum, acc[m]);
+            for (int e = 0; e < ROWS_LANE; ++e) xs[m][e] = c + e < p.cols ? to_f32(X[(m < n_tok ? m : 0) * p.ldx + c + e]) : 0.f;
+        }
+        const long long g = scales ? c / p.group : 0;
+        float s[ROWS_OF];
+#pragma unroll
+        for (int r = 0; r < ROWS_OF; ++r) s[r] = scales ? to_f32(scales[(r < rows ? r : 0) * p.n_groups + g]) : 1.f;
+#pragma unroll
+        for (int r = 0; r < ROWS_OF; ++r) {
+          float w[ROWS_LANE];
+#pragma unroll
+          for (int e = 0; e < ROWS_LANE; ++e) w[e] = lut[word[r] >> (4 * e) & 15u];
+#pragma unroll
+          for (int m = 0; m < TOK; ++m) {
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < ROWS_LANE; ++e) sum = fmaf(w[e], xs[m][e], sum);
+            acc[r][m] = fmaf(s[r], sum, acc[r][m]);
+          }
+          word[r] = next[r];
+        }
       }
     }
 #pragma unroll
-    for (int m = 0; m < TOK; ++m) {
+    for (int r = 0; r < ROWS_OF; ++r)
 #pragma unroll
-      for (int o = 16; o > 0; o >>= 1) acc[m] += __shfl_xor_sync(0xffffffffu, acc[m], o);
-      if (lane == 0 && m < n_tok) reinterpret_cast<T*>(p.Y)[(m0 + m) * p.ldy + n] = from_f32<T>(acc[m]);
+      for (int m = 0; m < TOK; ++m) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) acc[r][m] += __shfl_xor_sync(0xffffffffu, acc[r][m], o);
+        if (lane == 0) part[warp][r * TOK + m] = acc[r][m];
+      }
+    __syncthreads();
+    for (int i = threadIdx.x; i < sets * ROWS_OF * TOK; i += ROWS_BLOCK) {
+      const int set = i / (ROWS_OF * TOK), o = i % (ROWS_OF * TOK);
+      const long long n = (first + set) * ROWS_OF + o / TOK;
+      float v = 0.f;
+      for (int q = 0; q < split; ++q) v += part[set * split + q][o];
+      if (n < p.rows && o % TOK < n_tok) reinterpret_cast<T*>(p.Y)[(m0 + o % TOK) * p.ldy + n] = from_f32<T>(v);
     }
+    __syncthreads();
   }
 }
 
@@ -462,7 +516,6 @@ extern "C" int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_
   p.Y = Y; p.ldy = ldy;
   p.vec_x = (uintptr_t)X % 16 == 0 && ldx * tb % 16 == 0;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
-  const long long blocks = (rows + ROWS_BLOCK / 32 - 1) / (ROWS_BLOCK / 32);
   return with_type(type, [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
     if constexpr (sizeof(T) == 2) {
@@ -474,16 +527,28 @@ extern "C" int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_
       }
       if (tokens > 8) return codes_prompt(p, type, sms, st) == cudaSuccess ? IDKM_OK : IDKM_ERR_CUDA;
     }
-    constexpr int TOK = 4;
-    const long long tiles = (tokens + TOK - 1) / TOK;
+    const int TOK = tokens < 8 ? (int)tokens : 8;
+    const long long tiles = (tokens + TOK - 1) / TOK, quads = (rows + ROWS_OF - 1) / ROWS_OF;
+    // warps that share rows: until 16 a multiprocessor have work, as long as each has 256 columns
+    int split = 1;
+    while (split < ROWS_WARPS && quads * (tiles < 65535 ? tiles : 65535) * split < (long long)sms * 16 && cols > 256ll * split) split *= 2;
+    const long long blocks = (quads + ROWS_WARPS / split - 1) / (ROWS_WARPS / split);
     for (long long at = 0; at < tiles; at += 65535) {   // (a grid's second dimension)
       CodesParams q = p;
       q.X = reinterpret_cast<const T*>(X) + at * TOK * ldx;
       q.Y = reinterpret_cast<T*>(Y) + at * TOK * ldy;
       q.tokens = tokens - at * TOK;
       const dim3 grid((unsigned)(blocks < (long long)sms * 8 ? blocks : (long long)sms * 8), (unsigned)(tiles - at < 65535 ? tiles - at : 65535));
-      if (tokens == 1) idkm_codes_rows<T, 1><<<grid, ROWS_BLOCK, 0, st>>>(q);
-      else idkm_codes_rows<T, TOK><<<grid, ROWS_BLOCK, 0, st>>>(q);
+      switch (TOK) {
+        case 1: idkm_codes_rows<T, 1><<<grid, ROWS_BLOCK, 0, st>>>(q, split); break;
+        case 2: idkm_codes_rows<T, 2><<<grid, ROWS_BLOCK, 0, st>>>(q, split); break;
+        case 3: idkm_codes_rows<T, 3><<<grid, ROWS_BLOCK, 0, st>>>(q, split); break;
+        case 4: idkm_codes_rows<T, 4><<<grid, ROWS_BLOCK, 0, st>>>(q, split); break;
+        case 5: idkm_codes_rows<T, 5><<<grid, ROWS_BLOCK, 0, st>>>(q, split); break;
+        case 6: idkm_codes_rows<T, 6><<<grid, ROWS_BLOCK, 0, st>>>(q, split); break;
+        case 7: idkm_codes_rows<T, 7><<<grid, ROWS_BLOCK, 0, st>>>(q, split); break;
+        default: idkm_codes_rows<T, 8><<<grid, ROWS_BLOCK, 0, st>>>(q, split); break;
+      }
       if (cudaGetLastError() != cudaSuccess) return IDKM_ERR_CUDA;
     }
     return IDKM_OK;
