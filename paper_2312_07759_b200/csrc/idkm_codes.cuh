@@ -26,35 +26,34 @@ cudaError_t codes_prompt(const CodesParams& p, int type, int sms, cudaStream_t s
 __device__ __forceinline__ float code_scale(unsigned short u, __nv_bfloat16*) { return __uint_as_float((unsigned)u << 16); }
 __device__ __forceinline__ float code_scale(unsigned short u, __half*) { return __half2float(__ushort_as_half(u)); }
 
-// Eight 16-bit elements of a row from column k on, zeros past its end, whatever the row's alignment: from the one or two
-// 16-byte words that hold them.  (A word that holds one byte of the row lies in the row's pages.)
-__device__ __forceinline__ uint4 code_load8(const void* row, long long k, long long cols) {
-  uint4 r = make_uint4(0u, 0u, 0u, 0u);
-  if (k >= cols) return r;
-  const uintptr_t at = (uintptr_t)row + 2 * k, end = (uintptr_t)row + 2 * cols;
-  const uint4* word = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
-  const unsigned off = (unsigned)(at & 15u);
-  r = __ldg(word);
+// Eight 16-bit elements that begin `off` bytes (an even number) into the first of two words of memory; zeros from the `left`-th on.
+__device__ __forceinline__ uint4 code_align8(const uint4& a, const uint4& b, unsigned off, int left) {
+  unsigned w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
   if (off) {
-    uint4 h = make_uint4(0u, 0u, 0u, 0u);
-    if ((uintptr_t)(word + 1) < end) h = __ldg(word + 1);
-    unsigned w[8] = {r.x, r.y, r.z, r.w, h.x, h.y, h.z, h.w};
     if (off & 8u) { w[0] = w[2]; w[1] = w[3]; w[2] = w[4]; w[3] = w[5]; w[4] = w[6]; w[5] = w[7]; }
     if (off & 4u) { w[0] = w[1]; w[1] = w[2]; w[2] = w[3]; w[3] = w[4]; w[4] = w[5]; }
     if (off & 2u) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
     }
-    r = make_uint4(w[0], w[1], w[2], w[3]);
   }
-  if (k + 8 > cols) {
-    const int keep = (int)(cols - k);   // 1 to 7 elements
-    r.x &= keep >= 2 ? ~0u : 0xffffu;
-    r.y &= keep >= 4 ? ~0u : keep == 3 ? 0xffffu : 0u;
-    r.z &= keep >= 6 ? ~0u : keep == 5 ? 0xffffu : 0u;
-    r.w &= keep == 7 ? 0xffffu : 0u;
+  if (left < 8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] &= left >= 2 * i + 2 ? ~0u : left == 2 * i + 1 ? 0xffffu : 0u;
   }
-  return r;
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// Eight 16-bit elements of a row from column k on, zeros past its end, whatever the row's alignment: from the one or two
+// 16-byte words that hold them.  (A word that holds one byte of the row lies in the row's pages.)
+__device__ __forceinline__ uint4 code_load8(const void* row, long long k, long long cols) {
+  uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
+  if (k >= cols) return a;
+  const uintptr_t at = (uintptr_t)row + 2 * k, end = (uintptr_t)row + 2 * cols;
+  const uint4* word = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
+  const unsigned off = (unsigned)(at & 15u);
+  a = __ldg(word);
+  if (off && (uintptr_t)(word + 1) < end) b = __ldg(word + 1);
+  return code_align8(a, b, off, cols - k < 8 ? (int)(cols - k) : 8);
 }
 
 constexpr int CODE_POLLS = 1 << 22;   // (each waits for some time itself)

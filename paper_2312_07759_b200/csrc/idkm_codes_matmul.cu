@@ -144,9 +144,10 @@ __global__ void __launch_bounds__(ROWS_BLOCK) idkm_codes_rows(const __grid_const
 // rows that are free) in a fixed order, its scales come while the batch before is worked on, X lies there in the order the
 // threads read it.
 constexpr int FEW_WARPS = 16, FEW_BLOCK = 32 * FEW_WARPS, FEW_ROWS = 16;
+constexpr int FEW_ASK = 4;   // words of X that a thread has under way at the start
 constexpr int FEW_STRIPS = 2, FEW_CHUNK = 128 * FEW_STRIPS;
 constexpr int FEW_PITCH = FEW_WARPS * (FEW_CHUNK / 2) + 64, FEW_STAGE = FEW_ROWS * FEW_PITCH;   // (two rows' 64 bytes in different banks)
-constexpr int FEW_TABLE = 64 * 1024, FEW_SMEM = 227 * 1024 - 256, FEW_TILES = 16;               // tiles of a batch, at most
+constexpr int FEW_TABLE = 64 * 1024, FEW_SMEM = 227 * 1024 - 256, FEW_TILES = 8;                // tiles of a batch, at most (the first batch's scales are waited for)
 constexpr int FEW_BEFORE = FEW_TABLE - 1024, FEW_AFTER = FEW_SMEM - FEW_BEFORE - FEW_TABLE;     // shared memory starts at 1 KB
 
 __device__ __forceinline__ void few_mma(float (&c)[4], const unsigned (&a)[4], unsigned b0, unsigned b1, __nv_bfloat16*) {
@@ -189,6 +190,7 @@ __host__ __device__ __forceinline__ constexpr int few_column(int q, int t) {
 // a row of X there (two rows' 64 bytes in different banks).
 struct FewPlan {
   int chunks, tiles, stages, scale_words, xs;
+  unsigned x_words;     // i * x_words >> 32 is i over the 16-byte words of a row of X
   unsigned per_group;   // strip * per_group >> 20 is the group of a strip, where groups have whole strips (strips and a group's strips below 2^9)
   __host__ __device__ int scale_bytes() const { return 2 * tiles * FEW_ROWS * scale_words * 4; }   // of two batches
   __host__ __device__ int parts() const { return chunks < FEW_WARPS ? chunks : FEW_WARPS; }        // sums of a tile that meet
@@ -213,21 +215,12 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
   const int n_tiles = (int)((p.rows + FEW_ROWS - 1) / FEW_ROWS), n_groups = (int)p.n_groups;
   const int tile0 = (int)((long long)n_tiles * blockIdx.x / gridDim.x), tile1 = (int)((long long)n_tiles * (blockIdx.x + 1) / gridDim.x);
 
-  if (tid < 2 * f.stages) {
-    const int s = tid >> 1;
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"((tid & 1 ? empty : full) + 8 * s), "r"(tid & 1 ? FEW_WARPS : FEW_ROWS) : "memory");
-  }
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-  // the codebook is asked for first
-  const unsigned short* c = reinterpret_cast<const unsigned short*>(p.C);
-  unsigned lo = 0u, hi = 0u;
-  if (tid < 256) {
-    if ((tid & 15) < p.k) lo = __ldg(c + (tid & 15));
-    if ((tid >> 4) < p.k) hi = __ldg(c + (tid >> 4));
-  }
-  __syncthreads();
-
   if (warp == FEW_WARPS) {   // the copies: a lane a row
+    if (lane < 2 * f.stages)
+      asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"((lane & 1 ? empty : full) + 8 * (lane >> 1)), "r"(lane & 1 ? FEW_WARPS : FEW_ROWS) : "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    asm volatile("bar.arrive 2, %0;" ::"n"(FEW_BLOCK + 32) : "memory");   // (the barriers are ready)
     if (lane < FEW_ROWS) {
       int stage = 0, turn = 0;
       bool filled = false;   // every stage has been filled once
@@ -279,50 +272,60 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
   if (SCALED) copy_scales(tile0, 0);
-  const int words = chunks * (FEW_CHUNK / 8), n_words = tokens * words;   // 16-byte words of a row of X
-  auto place_x = [&](int i, bool load, uint4& x) {
-    const int m = i / words, v = i - m * words, place = v & 15;   // place 4 q + t of a strip: for word q of thread t
-    if (load) x = code_load8(reinterpret_cast<const T*>(p.X) + m * p.ldx, (long long)(v >> 4) * 128 + 8 * few_column<Q>(place >> 2, place & 3), p.cols);
-    else *reinterpret_cast<uint4*>(row_of(m) + v * 16) = x;
-  };
-  {
-    uint4 first[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-      if (tid + u * FEW_BLOCK < n_words) place_x(tid + u * FEW_BLOCK, true, first[u]);
-    if (tid < 256) {
-      const unsigned both = lo | hi << 16;
-#pragma unroll
-      for (int q = 0; q < 8; ++q)   // (lanes at different places of their rows: in different banks)
-        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(table + tid * 256 + ((q + lane) & 7) * 16), "r"(both) : "memory");
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-      if (tid + u * FEW_BLOCK < n_words) place_x(tid + u * FEW_BLOCK, false, first[u]);
+  // The codebook, and X by 16-byte words, whatever its rows' alignment: the one or two words of memory that hold eight elements (one
+  // that holds a byte of the row lies in its pages).  All that a thread loads it asks for before it looks at the first.
+  const unsigned short* c = reinterpret_cast<const unsigned short*>(p.C);
+  unsigned lo = 0u, hi = 0u;
+  if (tid < 256) {
+    if ((tid & 15) < p.k) lo = __ldg(c + (tid & 15));
+    if ((tid >> 4) < p.k) hi = __ldg(c + (tid >> 4));
   }
-  for (int i = tid + 2 * FEW_BLOCK; i < n_words; i += 4 * FEW_BLOCK) {
-    uint4 some[4];
+  const int words = chunks * (FEW_CHUNK / 8), n_words = tokens * words;
+  auto column_of = [&](int v) { return (v >> 4) * 128 + 8 * few_column<Q>((v >> 2) & 3, v & 3); };   // place 4 q + t of a strip: for word q of thread t
+  auto ask = [&](int i, uint4& a, uint4& b) {
+    const int m = (int)__umulhi((unsigned)i, f.x_words), k = column_of(i - m * words);
+    const uintptr_t row = (uintptr_t)(reinterpret_cast<const T*>(p.X) + m * p.ldx), at = row + 2 * k, end = row + 2 * p.cols;
+    const uintptr_t word = at & ~(uintptr_t)15;
+    const int first = i < n_words && at < end, second = first && (at & 15) && word + 16 < end;
+    a = b = make_uint4(0u, 0u, 0u, 0u);
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %9, 0;\n\tsetp.ne.b32 q, %10, 0;\n\t@p ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%8];\n\t"
+                 "@q ld.global.nc.v4.u32 {%4, %5, %6, %7}, [%8+16];\n\t}"
+                 : "+r"(a.x), "+r"(a.y), "+r"(a.z), "+r"(a.w), "+r"(b.x), "+r"(b.y), "+r"(b.z), "+r"(b.w) : "l"(word), "r"(first), "r"(second));
+  };
+  auto place = [&](int i, const uint4& a, const uint4& b) {
+    if (i >= n_words) return;
+    const int m = (int)__umulhi((unsigned)i, f.x_words), v = i - m * words;
+    const unsigned off = (unsigned)((uintptr_t)(reinterpret_cast<const T*>(p.X) + m * p.ldx) & 15u);   // (columns by eights: the row's)
+    *reinterpret_cast<uint4*>(row_of(m) + v * 16) = code_align8(a, b, off, (int)p.cols - column_of(v));
+  };
+  for (int i0 = tid; i0 < n_words; i0 += FEW_ASK * FEW_BLOCK) {
+    uint4 a[FEW_ASK], b[FEW_ASK];
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (i + u * FEW_BLOCK < n_words) place_x(i + u * FEW_BLOCK, true, some[u]);
+    for (int u = 0; u < FEW_ASK; ++u) ask(i0 + u * FEW_BLOCK, a[u], b[u]);
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (i + u * FEW_BLOCK < n_words) place_x(i + u * FEW_BLOCK, false, some[u]);
+    for (int u = 0; u < FEW_ASK; ++u) place(i0 + u * FEW_BLOCK, a[u], b[u]);
+  }
+  if (tid < 256) {
+    const unsigned both = lo | hi << 16;
+#pragma unroll
+    for (int q = 0; q < 8; ++q)   // (lanes at different places of their rows: in different banks)
+      asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(table + tid * 256 + ((q + lane) & 7) * 16), "r"(both) : "memory");
   }
   auto meet = [] { asm volatile("bar.sync 1, %0;" ::"n"(FEW_BLOCK) : "memory"); };
   asm volatile("cp.async.wait_group 0;" ::: "memory");
-  meet();
+  asm volatile("bar.sync 2, %0;" ::"n"(FEW_BLOCK + 32) : "memory");
 
   // (a value that is there after the barrier only: the lookups, which may be moved about, stay behind it)
   unsigned mine;
   asm volatile("or.b32 %0, %1, %2;" : "=r"(mine) : "r"(table), "r"((unsigned)lane * 4u) : "memory");
   // this thread's row of X; threads of columns that X has no row for keep their zeros
-  unsigned x_row[NT], x_there[NT];
+  const unsigned char* x_row[NT];
+  bool x_there[NT];
   uint4 x[2][NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
     x_there[n] = n * 8 + gid < tokens;
-    x_row[n] = (unsigned)__cvta_generic_to_shared(row_of(min(n * 8 + gid, tokens - 1))) + tig * 16;
+    x_row[n] = row_of(min(n * 8 + gid, tokens - 1)) + tig * 16;
     x[0][n] = x[1][n] = make_uint4(0u, 0u, 0u, 0u);
   }
   auto first_scale = [&](int strip) { return Q > 1 ? strip * Q : (int)((unsigned)strip * f.per_group >> 20); };
@@ -360,7 +363,7 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
         unsigned scale_of[2];   // the scales of this thread's rows
         if (SCALED) {
           const int r = tile * FEW_ROWS + gid;
-          const unsigned odd = (unsigned)(((uintptr_t)p.scales >> 1) + ((long long)batch * FEW_ROWS + r) * n_groups) & 1u;   // (8 rows on: the same)
+          const unsigned odd = ((unsigned)((uintptr_t)p.scales >> 1) + ((unsigned)r & (unsigned)n_groups)) & 1u;   // (16 and 8 rows on: the same)
           scale_of[0] = raw + (unsigned)(turn * (f.scale_bytes() / 2) + r * f.scale_words * 4) + 2 * odd;
           scale_of[1] = scale_of[0] + 8 * f.scale_words * 4;
         }
@@ -372,9 +375,7 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
           for (int q = 0; q < 4; ++q) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
-              asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t@p ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];\n\t}"
-                           : "+r"(x[q & 1][n].x), "+r"(x[q & 1][n].y), "+r"(x[q & 1][n].z), "+r"(x[q & 1][n].w)
-                           : "r"(x_row[n] + x_at + u * 256 + q * 64), "r"(x_there[n]));
+              if (x_there[n]) x[q & 1][n] = *reinterpret_cast<const uint4*>(x_row[n] + x_at + u * 256 + q * 64);
             const unsigned w0 = q == 0 ? w[u][0].x : q == 1 ? w[u][0].y : q == 2 ? w[u][0].z : w[u][0].w;
             const unsigned w1 = q == 0 ? w[u][1].x : q == 1 ? w[u][1].y : q == 2 ? w[u][1].z : w[u][1].w;
 #pragma unroll
@@ -461,6 +462,7 @@ inline bool few_plan(const CodesParams& p, FewPlan& f) {
   if (p.tokens > 16 || p.rows > INT32_MAX - FEW_ROWS || p.cols > FEW_AFTER / 2) return false;
   f.chunks = (int)((p.cols + FEW_CHUNK - 1) / FEW_CHUNK);
   f.xs = f.chunks * (2 * FEW_CHUNK) + 64;
+  f.x_words = (unsigned)((0x100000000ull + f.chunks * (FEW_CHUNK / 8) - 1) / (f.chunks * (FEW_CHUNK / 8)));
   if (p.group >= 128) {
     const long long per = p.group / 128;   // (longer than a row: one group)
     if (2 * f.chunks >= 512) return false;
@@ -471,7 +473,8 @@ inline bool few_plan(const CodesParams& p, FewPlan& f) {
     for (f.tiles = FEW_TILES; f.tiles >= 1; f.tiles /= 2) {
       if (2 * f.tiles * f.parts() * FEW_ROWS * (int)p.tokens * 4 > FEW_TABLE / 2) continue;
       const int left = FEW_BEFORE - 1024 - f.scale_bytes();   // (shared memory starts at up to 2 KB)
-      if (left >= 0 && left / f.xs + (FEW_AFTER - f.stages * FEW_STAGE) / f.xs >= p.tokens) return true;
+      const int after = FEW_AFTER - f.stages * FEW_STAGE;
+      if (left >= 0 && after >= 0 && left / f.xs + after / f.xs >= p.tokens) return true;
     }
   return false;
 }

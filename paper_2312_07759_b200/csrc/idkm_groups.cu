@@ -151,7 +151,7 @@ __device__ __forceinline__ unsigned groups_codes(const GroupsTable& t, const flo
       node[e] = __funnelshift_l(__float_as_uint(d[e]), node[e], 1);
     }
 #pragma unroll
-    for (int e = 0; e < GROUPS_LANE; e += 2) near = fminf(near, fminf(fabsf(d[e]), fabsf(d[e + 1])));
+    for (int e = 0; e < GROUPS_LANE; e += 2) asm("min.abs.f32 %0, %0, %1, %2;" : "+f"(near) : "f"(d[e]), "f"(d[e + 1]));
   }
   unsigned out = 0u;
   if (t.sorted) {
@@ -217,7 +217,7 @@ __device__ __forceinline__ unsigned groups_keep(unsigned codes, int c, int cols)
   return c + GROUPS_LANE <= cols ? codes : c >= cols ? 0u : codes & ((1u << (4 * (cols - c))) - 1u);
 }
 
-// The larger of two sizes; a NaN stays.
+// The larger of two sizes (what it takes may have a sign); a NaN stays.
 __device__ __forceinline__ float groups_larger(float a, float b) {
   float r;
   asm("max.NaN.xorsign.abs.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
@@ -226,13 +226,13 @@ __device__ __forceinline__ float groups_larger(float a, float b) {
 __device__ __forceinline__ float groups_largest(const float (&w)[GROUPS_LANE]) {
   float most = 0.f;
 #pragma unroll
-  for (int e = 0; e < GROUPS_LANE; ++e) most = groups_larger(most, w[e]);
+  for (int e = 0; e < GROUPS_LANE; e += 2) asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(w[e]), "f"(w[e + 1]));
   return most;
 }
 
 // Groups of 32, 64, 128 or 256 weights: L = g / 8 neighbouring lanes share one.  A warp takes GROUPS_PIECES pieces of 256 weights of a
 // row at a time, all of them asked for before the first is looked at.
-constexpr int GROUPS_PIECES = 4;
+constexpr int GROUPS_PIECES = 2;   // (1, 3, 4: 114, 104, 105 us where 2 take 103)
 template <class TW>
 struct GroupsRaw {   // a lane's eight weights as they lie in memory
   uint4 v[GROUPS_LANE / Vec16<TW>::N];
@@ -251,7 +251,7 @@ __device__ __noinline__ GroupsRaw<TW> groups_edge(const TW* row, int c, int cols
   return r;
 }
 template <class TW, class T>
-__global__ void __launch_bounds__(GROUPS_BLOCK, 3) idkm_groups_short(const __grid_constant__ GroupsParams p) {
+__global__ void __launch_bounds__(GROUPS_BLOCK, 4) idkm_groups_short(const __grid_constant__ GroupsParams p) {
   constexpr int N = Vec16<TW>::N, V = GROUPS_LANE / N;
   __shared__ GroupsTable t;
   const int lane = threadIdx.x & 31, L = p.group / GROUPS_LANE, shift = __ffs(p.group) - 1, cols = p.cols, span = GROUPS_PIECES * GROUPS_WARP;
@@ -396,7 +396,7 @@ extern "C" int idkm_assign_groups(const void* W, int w_type, int64_t rows, int64
   p.vec_out = (uintptr_t)Wq_out % 16 == 0 && cols * wb % 16 == 0;
   const bool shorter = p.group <= GROUPS_WARP && GROUPS_WARP % p.group == 0;
   const long long per_row = (cols + GROUPS_PIECES * GROUPS_WARP - 1) / (GROUPS_PIECES * GROUPS_WARP);
-  const long long jobs = shorter ? (rows * per_row + GROUPS_BLOCK / 32 - 1) / (GROUPS_BLOCK / 32) : rows * p.n_groups, most = (long long)sms * (shorter ? 3 : 8);
+  const long long jobs = shorter ? (rows * per_row + GROUPS_BLOCK / 32 - 1) / (GROUPS_BLOCK / 32) : rows * p.n_groups, most = (long long)sms * (shorter ? 4 : 8);
   const int grid = (int)(jobs < most ? jobs : most);
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   return with_type(w_type, [&](auto* w) {
