@@ -190,6 +190,8 @@ __host__ __device__ __forceinline__ constexpr int few_column(int q, int t) {
 // a row of X there (two rows' 64 bytes in different banks).
 struct FewPlan {
   int chunks, tiles, stages, scale_words, xs;
+  int per_block, extra;          // tiles of every block, blocks that have one more
+  unsigned scale_inv;   // i * scale_inv >> 32 is i over the words that a row's scales may touch
   unsigned x_words;     // i * x_words >> 32 is i over the 16-byte words of a row of X
   unsigned per_group;   // strip * per_group >> 20 is the group of a strip, where groups have whole strips (strips and a group's strips below 2^9)
   __host__ __device__ int scale_bytes() const { return 2 * tiles * FEW_ROWS * scale_words * 4; }   // of two batches
@@ -212,8 +214,8 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
   const int before = min(((int)(table - raw) - f.scale_bytes()) / f.xs, tokens);   // rows of X that lie before the table
   auto row_of = [&](int m) { return m < before ? few_raw + f.scale_bytes() + m * f.xs : at_table + FEW_TABLE + f.stages * FEW_STAGE + (m - before) * f.xs; };
   const int code_bytes = (int)((p.cols + 31) / 32) * 16;
-  const int n_tiles = (int)((p.rows + FEW_ROWS - 1) / FEW_ROWS), n_groups = (int)p.n_groups;
-  const int tile0 = (int)((long long)n_tiles * blockIdx.x / gridDim.x), tile1 = (int)((long long)n_tiles * (blockIdx.x + 1) / gridDim.x);
+  const int n_groups = (int)p.n_groups;
+  const int tile0 = (int)blockIdx.x * f.per_block + min((int)blockIdx.x, f.extra), tile1 = tile0 + f.per_block + ((int)blockIdx.x < f.extra ? 1 : 0);
 
   if (warp == FEW_WARPS) {   // the copies: a lane a row
     if (lane < 2 * f.stages)
@@ -262,16 +264,17 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
 
   // scales of a batch, by words; a row's may begin in the middle of one.  (A word that holds one byte of them lies in their pages.)
   auto copy_scales = [&](int batch, int turn) {
-    const long long r0 = (long long)batch * FEW_ROWS, rows = min((long long)min(batch + f.tiles, tile1) * FEW_ROWS, p.rows) - r0;
+    const long long r0 = (long long)batch * FEW_ROWS;
+    const int rows = (int)min((long long)(min(batch + f.tiles, tile1) - batch) * FEW_ROWS, p.rows - r0), words = max(n_groups / 2 + 1, 2);   // the most words that a row's touch
     const unsigned to = raw + (unsigned)(turn * (f.scale_bytes() / 2));
-    for (int r = warp; r < (int)rows; r += FEW_WARPS) {
-      const uintptr_t at = (uintptr_t)p.scales + 2 * (r0 + r) * p.n_groups;
-      for (uintptr_t word = (at & ~(uintptr_t)3) + 4 * lane, place = to + (r * f.scale_words + lane) * 4; word < at + 2 * n_groups; word += 128, place += 128)
-        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((unsigned)place), "l"(word) : "memory");
+    const uintptr_t from = (uintptr_t)p.scales + 2 * r0 * p.n_groups;
+    for (int i = tid; i < rows * words; i += FEW_BLOCK) {
+      const int r = (int)__umulhi((unsigned)i, f.scale_inv), w = i - r * words;
+      const uintptr_t at = from + 2 * (unsigned)(r * n_groups), word = (at & ~(uintptr_t)3) + 4 * w;
+      if (word < at + 2 * n_groups) asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to + (unsigned)(r * f.scale_words + w) * 4u), "l"(word) : "memory");
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   };
-  if (SCALED) copy_scales(tile0, 0);
   // The codebook, and X by 16-byte words, whatever its rows' alignment: the one or two words of memory that hold eight elements (one
   // that holds a byte of the row lies in its pages).  All that a thread loads it asks for before it looks at the first.
   const unsigned short* c = reinterpret_cast<const unsigned short*>(p.C);
@@ -298,12 +301,19 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
     const unsigned off = (unsigned)((uintptr_t)(reinterpret_cast<const T*>(p.X) + m * p.ldx) & 15u);   // (columns by eights: the row's)
     *reinterpret_cast<uint4*>(row_of(m) + v * 16) = code_align8(a, b, off, (int)p.cols - column_of(v));
   };
-  for (int i0 = tid; i0 < n_words; i0 += FEW_ASK * FEW_BLOCK) {
+  {
     uint4 a[FEW_ASK], b[FEW_ASK];
 #pragma unroll
-    for (int u = 0; u < FEW_ASK; ++u) ask(i0 + u * FEW_BLOCK, a[u], b[u]);
+    for (int u = 0; u < FEW_ASK; ++u) ask(tid + u * FEW_BLOCK, a[u], b[u]);
+    if (SCALED) copy_scales(tile0, 0);   // (the first batch's scales come meanwhile)
+    for (int i0 = tid;;) {
 #pragma unroll
-    for (int u = 0; u < FEW_ASK; ++u) place(i0 + u * FEW_BLOCK, a[u], b[u]);
+      for (int u = 0; u < FEW_ASK; ++u) place(i0 + u * FEW_BLOCK, a[u], b[u]);
+      i0 += FEW_ASK * FEW_BLOCK;
+      if (i0 >= n_words) break;
+#pragma unroll
+      for (int u = 0; u < FEW_ASK; ++u) ask(i0 + u * FEW_BLOCK, a[u], b[u]);
+    }
   }
   if (tid < 256) {
     const unsigned both = lo | hi << 16;
@@ -462,6 +472,8 @@ inline bool few_plan(const CodesParams& p, FewPlan& f) {
   if (p.tokens > 16 || p.rows > INT32_MAX - FEW_ROWS || p.cols > FEW_AFTER / 2) return false;
   f.chunks = (int)((p.cols + FEW_CHUNK - 1) / FEW_CHUNK);
   f.xs = f.chunks * (2 * FEW_CHUNK) + 64;
+  const unsigned long long scale_words = p.n_groups > 1 ? p.n_groups / 2 + 1 : 2;
+  f.scale_inv = (unsigned)((0x100000000ull + scale_words - 1) / scale_words);
   f.x_words = (unsigned)((0x100000000ull + f.chunks * (FEW_CHUNK / 8) - 1) / (f.chunks * (FEW_CHUNK / 8)));
   if (p.group >= 128) {
     const long long per = p.group / 128;   // (longer than a row: one group)
@@ -480,12 +492,15 @@ inline bool few_plan(const CodesParams& p, FewPlan& f) {
 }
 
 template <class T, int Q, int NT, bool SCALED>
-cudaError_t few_launch(const CodesParams& p, const FewPlan& f, int sms, cudaStream_t st) {
+cudaError_t few_launch(const CodesParams& p, FewPlan f, int sms, cudaStream_t st) {
   static PerDevice limit;
   const cudaError_t rc = allow_smem(limit, idkm_codes_few<T, Q, NT, SCALED>, FEW_SMEM);
   if (rc != cudaSuccess) return rc;
   const long long tiles = (p.rows + FEW_ROWS - 1) / FEW_ROWS;
-  idkm_codes_few<T, Q, NT, SCALED><<<(int)(tiles < sms ? tiles : sms), FEW_BLOCK + 32, FEW_SMEM, st>>>(p, f);
+  const int blocks = (int)(tiles < sms ? tiles : sms);
+  f.per_block = (int)(tiles / blocks);
+  f.extra = (int)(tiles % blocks);
+  idkm_codes_few<T, Q, NT, SCALED><<<blocks, FEW_BLOCK + 32, FEW_SMEM, st>>>(p, f);
   return cudaGetLastError();
 }
 
