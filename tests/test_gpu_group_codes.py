@@ -315,3 +315,96 @@ def test_the_operators_together():
     rdW, rdC, _, _ = R.backward(W64, G64, Ct, float(np.float32(tau_w)), S, F, adj_max_iter=20)
     assert np.abs(dC.cpu().numpy() - rdC).max() < 2e-3 * np.abs(rdC).max()
     assert np.linalg.norm(dW.cpu().numpy() - rdW) < 3e-3 * np.linalg.norm(rdW)
+
+
+@pytest.mark.parametrize("t", ["bfloat16", "float16"])
+@pytest.mark.parametrize("tokens,rows,cols,group", [(1, 21, 51000, 128), (1, 5, 70000, 65536), (2, 37, 33000, 32), (8, 33, 12300, 64), (8, 50, 9000, 32),
+                                                    (12, 40, 9000, 128), (16, 257, 4096, 256), (16, 30, 5200, 32), (10, 3000, 260, 0), (3, 70, 16384, 1 << 20),
+                                                    (40, 513, 70, 32), (31, 2000, 1000, 640)])
+def test_products_between_the_kernels(t, tokens, rows, cols, group):
+    """Rows that fit into a multiprocessor's memory with the stages, with fewer of them, and not at all; groups longer than that."""
+    import torch
+    from paper_2312_07759_b200 import binding as B
+    X, codes, C, s = _case(torch, tokens, rows, cols, group, t)
+    ref = B.matmul_codes(X, codes, C, s, group)
+    _check_product(torch, ref, X, codes, C, s, group)
+    wide = torch.full((tokens, cols + 3), float("nan"), device="cuda", dtype=X.dtype)
+    wide[:, 3:] = X
+    _check_product(torch, B.matmul_codes(wide[:, 3:], codes, C, s, group), X, codes, C, s, group)
+
+
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("rows,cols,group", [(40, 4099, 32), (17, 513, 64), (9, 1025, 128)])
+def test_products_with_scales_and_rows_anywhere(t, rows, cols, group):
+    """Scales, codebook and X that begin at any element of a larger tensor (odd numbers of groups a row among them)."""
+    import torch
+    from paper_2312_07759_b200 import binding as B
+    for tokens in (1, 6, 70):
+        X, codes, C, s = _case(torch, tokens, rows, cols, group, t)
+        ref = B.matmul_codes(X, codes, C, s, group)
+        for at in (1, 2, 5):
+            flat = torch.full((s.numel() + 8,), float("nan"), device="cuda", dtype=s.dtype)
+            flat[at:at + s.numel()] = s.flatten()
+            book = torch.full((24,), float("nan"), device="cuda", dtype=s.dtype)
+            book[at:at + 16] = C
+            got = B.matmul_codes(X, codes, book[at:at + 16], flat[at:at + s.numel()].view(s.shape), group)
+            assert torch.equal(got, ref)
+
+
+@pytest.mark.parametrize("t", ["bfloat16", "float32"])
+def test_guard_words_around_products(t):
+    """Every byte outside the result stays as it was, whichever kernel takes the product."""
+    import torch
+    from paper_2312_07759_b200 import binding as B
+    for tokens, rows, cols in [(1, 1, 1), (1, 33, 300), (5, 1001, 640), (16, 129, 256), (18, 257, 200), (150, 131, 129)]:
+        X, codes, C, s = _case(torch, tokens, rows, cols, 64, t)
+        room = torch.full((tokens * rows + 4096,), 3.0, device="cuda", dtype=X.dtype)
+        out = room[2048:2048 + tokens * rows].view(tokens, rows)
+        B.matmul_codes(X, codes, C, s, 64, out=out)
+        _check_product(torch, out, X, codes, C, s, 64)
+        assert torch.all(room[:2048] == 3.0) and torch.all(room[2048 + tokens * rows:] == 3.0)
+
+
+def test_guard_words_around_the_export():
+    import torch
+    from paper_2312_07759_b200 import binding as B
+    C = torch.linspace(-1, 1, 16, device="cuda").bfloat16()
+    for rows, cols, group in [(1, 1, 32), (3, 33, 32), (7, 1000, 128), (2, 5000, 384), (300, 257, 64)]:
+        W = torch.randn(rows, cols, device="cuda")
+        pitch, n = (cols + 31) // 32 * 16, -(-cols // group)
+        codes = torch.full((rows * pitch + 512,), 0xA5, device="cuda", dtype=torch.uint8)
+        scales = torch.full((rows * n + 512,), 3.0, device="cuda", dtype=torch.bfloat16)
+        Wq = torch.full((rows * cols + 512,), 3.0, device="cuda")
+        rc = B.lib.idkm_assign_groups(W.data_ptr(), 0, rows, cols, cols, C.data_ptr(), 16, 1, group, codes[256:].data_ptr(), scales[256:].data_ptr(),
+                                      Wq[256:].data_ptr(), None)
+        assert rc == B.OK
+        torch.cuda.synchronize()
+        want = B.assign_groups(W, C, group, want_Wq=True)
+        for room, got, v in ((codes, want[0], 0xA5), (scales, want[1], 3.0), (Wq, want[2], 3.0)):
+            k = got.numel()
+            assert torch.equal(room[256:256 + k], got.flatten()) and torch.all(room[:256] == v) and torch.all(room[256 + k:] == v)
+
+
+def test_calls_at_once_from_threads():
+    """Two host threads, a stream each: every call gets its own result."""
+    import threading
+    import torch
+    from paper_2312_07759_b200 import binding as B
+    work = [_case(torch, m, 700, 1024, 128, "bfloat16", seed=i) for i, m in enumerate((1, 4, 16, 100))]
+    refs = [B.matmul_codes(X, codes, C, s, 128) for X, codes, C, s in work]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(i):
+        stream = torch.cuda.Stream()
+        for k in range(60):
+            X, codes, C, s = work[(i + k) % 4]
+            Y = B.matmul_codes(X, codes, C, s, 128, stream=stream)
+            stream.synchronize()
+            if not torch.equal(Y, refs[(i + k) % 4]):
+                wrong.append((i, k))
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert not wrong
