@@ -10,11 +10,11 @@
 // part, which every block has whole but for the entries' products, for which it takes the entries of its own part of the row;
 // blocks send theirs into the others' shared memory.  Then q_v = e_v exp((m - M) / tau) / S: an element costs one exponential, 2
 // or 4 bytes in, as many out.  Entries' places are written again after the dense part.
-// What bounds it: at 4096 x 32000 bf16 logits 124 us, 4.3 TB/s; 920 instructions of a warp for 64 elements a thread (about 360 for
-// the elements, the rest reductions and bookkeeping of a row) keep the issue slots half busy, the chain of a row's two barriers and
-// one exchange the other half.  Measured: 4 vectors a thread and twice the blocks 269 us (a row's bookkeeping is per warp),
-// exponentials computed twice instead of kept, for three blocks of a multiprocessor instead of two, 147 us; one block of 512
-// threads instead of two of 256 131 us.  The gradient alone is streamed: 1021 x 100003 fp16 65 us, 6.3 TB/s, as fast as a copy.
+// What bounds it: at 4096 x 32000 bf16 logits 111 us, 4.7 TB/s: the elements' instructions (about 6 each) and the chain of a row's
+// two barriers and one exchange, behind which the next row's entries are prepared (8 us).  Measured when this took 124 us: 4 vectors
+// a thread and twice the blocks 269 us (a row's bookkeeping is per warp), exponentials computed twice instead of kept, for three blocks
+// of a multiprocessor instead of two, 147, one block of 512 threads instead of two of 256 131, warps' parts joined by every thread
+// from shared memory instead of by lanes 136.  The gradient alone is streamed: 1021 x 100003 fp16 66 us, 6.2 TB/s, as fast as a copy.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -71,10 +71,10 @@ __device__ __forceinline__ float distill_scale(float m, float top, float c2) {
 // A part that another scale multiplies: 0 stays 0 whatever the scale; NaN stays.
 __device__ __forceinline__ float distill_scaled(float s, float f) { return s == 0.f ? 0.f : s * f; }
 
-__device__ __forceinline__ float distill_warp_max(float x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, o));
-  return x;
+__device__ __forceinline__ float distill_warp_max(float x) {   // (NaN aside)
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));
+  return r;
 }
 __device__ __forceinline__ float distill_warp_sum(float x) {
 #pragma unroll
@@ -86,12 +86,7 @@ __device__ __forceinline__ float distill_warp_sum(float x) {
 template <int WARPS>
 __device__ __forceinline__ DistillPart distill_join(DistillPart a, float c2) {
   const float inf = __int_as_float(0x7f800000);
-  float M = a.m, T = a.tm;
-#pragma unroll
-  for (int o = WARPS >> 1; o > 0; o >>= 1) {
-    M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    T = fmaxf(T, __shfl_xor_sync(0xffffffffu, T, o));
-  }
+  const float M = distill_warp_max(a.m), T = distill_warp_max(a.tm);
   const float g = distill_scale(a.tm, T, c2);
   a.s = distill_scaled(a.s, distill_scale(a.m, M, c2));
   a.ts = distill_scaled(a.ts, g);
@@ -102,8 +97,8 @@ __device__ __forceinline__ DistillPart distill_join(DistillPart a, float c2) {
     a.ts += __shfl_xor_sync(0xffffffffu, a.ts, o);
     a.ta += __shfl_xor_sync(0xffffffffu, a.ta, o);
   }
-  a.m = __shfl_sync(0xffffffffu, M, 0);
-  a.tm = __shfl_sync(0xffffffffu, T, 0);
+  a.m = M;
+  a.tm = T;
   a.s = __shfl_sync(0xffffffffu, a.s, 0);
   a.ts = __shfl_sync(0xffffffffu, a.ts, 0);
   a.ta = __shfl_sync(0xffffffffu, a.ta, 0);
@@ -351,18 +346,6 @@ __global__ void __launch_bounds__(BLOCK, 512 / BLOCK) idkm_distill_rows(const __
   for (int turn = 0; row < p.rows; row += n_clusters, turn ^= 1) {
     const DistillGrid<T> g(p, row);
     const long long next = row + n_clusters;
-    if (next < p.rows) {
-      if (warp * 32 < p.top) {
-        distill_entry(p, raw, at1, t1);
-        raw = distill_raw(p, next + n_clusters, tid);
-        const DistillGrid<T> g1(p, next);
-        if (has(g1, at1)) own1 = g1.z[at1];
-      } else {
-        at1 = -1;
-        t1 = none;
-      }
-      if (MODE == DISTILL_STEP && p.weight) w1 = p.weight[next];
-    }
     const bool mine = has(g, at);
     int entered = -1;
     if (tid < p.top) {
@@ -451,6 +434,19 @@ __global__ void __launch_bounds__(BLOCK, 512 / BLOCK) idkm_distill_rows(const __
       if (entered >= 0) s_table[entered] = -1;
     }
     if (MODE == DISTILL_STEP && tid == 0) s_twice[turn ^ 1] = 0;
+    // while the parts are on their way: the next row's entries, the one after asked for
+    if (next < p.rows) {
+      if (warp * 32 < p.top) {
+        distill_entry(p, raw, at1, t1);
+        raw = distill_raw(p, next + n_clusters, tid);
+        const DistillGrid<T> g1(p, next);
+        if (has(g1, at1)) own1 = g1.z[at1];
+      } else {
+        at1 = -1;
+        t1 = none;
+      }
+      if (MODE == DISTILL_STEP && p.weight) w1 = p.weight[next];
+    }
     if (parts > 1) {
       bool ok = lost;
       for (int i = 0; i < DISTILL_POLLS && !ok; ++i) {
