@@ -408,3 +408,17 @@ def test_calls_at_once_from_threads():
     [t.start() for t in threads]
     [t.join() for t in threads]
     assert not wrong
+
+
+@pytest.mark.parametrize("t", ["bfloat16", "float16"])
+@pytest.mark.parametrize("tokens,rows,cols,group", [(16, 40, 20000, 32), (9, 535, 11392, 64), (16, 300, 8197, 128), (8, 100, 28672, 0), (12, 50, 40001, 3200),
+                                                    (16, 20, 140000, 65664), (3, 33, 70001, 35072), (16, 39000, 2900, 128), (5, 17, 131072, 32),
+                                                    (1, 2500, 90000, 256)])
+def test_products_whose_columns_come_in_parts(t, tokens, rows, cols, group):
+    """X that one multiprocessor cannot hold: groups that end where a part does, in its middle, and that span several."""
+    import torch
+    from paper_2312_07759_b200 import binding as B
+    X, codes, C, s = _case(torch, tokens, rows, cols, group, t)
+    ref = B.matmul_codes(X, codes, C, s, group)
+    _check_product(torch, ref, X, codes, C, s, group)
+    assert torch.equal(B.matmul_codes(X, codes, C, s, group), ref)
