@@ -318,8 +318,8 @@ size_t idkm_codes_bytes(int64_t m, int k);   /* ceil(m * idkm_code_bits(k) / 8);
  * [rows][cols], contiguous, or NULL) receives s c_j, multiplied in fp32 and rounded to w_type.  Codebook entries that are not
  * finite are never the nearest and have no part in max_j|c_j|.  A group with a NaN or an infinity, or whose scale leaves the
  * range of `type`, gets a scale that is not finite and codes 0; where s is 0 (weights all 0, or too small for `type`) the codes
- * are 0 as well.  codes_out 16-byte aligned; the others to their elements.  No context, no workspace; asynchronous on
- * cuda_stream; outputs may not overlap inputs.  Returns IDKM_OK, IDKM_ERR_NULL, IDKM_ERR_UNSUPPORTED (k, types, group),
+ * are 0 as well.  codes_out 16-byte aligned; the others to their elements; up to 2^31 - 4097 columns.  No context, no workspace;
+ * asynchronous on cuda_stream; outputs may not overlap inputs.  Returns IDKM_OK, IDKM_ERR_NULL, IDKM_ERR_UNSUPPORTED (k, types, group),
  * IDKM_ERR_SHAPE, IDKM_ERR_PARAM, IDKM_ERR_ALIGN or IDKM_ERR_CUDA.
  */
 int idkm_assign_groups(const void* W, int w_type, int64_t rows, int64_t cols, int64_t ldw, const void* C, int k, int type,
@@ -335,8 +335,9 @@ int64_t idkm_group_codes_pitch(int64_t cols);   /* 16 ceil(cols / 32); 0 for col
  * idkm_assign for a layer of 5 <= k <= 16 scalar centroids and rows of a multiple of 32 weights).  Products and sums are in
  * fp32, the scale multiplies the fp32 sum of its group, and Y is rounded once; the order of the sums depends on the shape
  * alone.  C must be finite; a code that names no entry stands for 0.  codes 16-byte aligned, the others to their elements
- * (X is read fastest from 16-byte-aligned rows).  Y may not overlap an input.  No context, no workspace; asynchronous on
- * cuda_stream.  Returns as idkm_assign_groups.
+ * (X is read fastest from 16-byte-aligned rows).  group as above, or any number >= cols: one scale a row.  Tokens, rows and columns
+ * up to 2^31 - 4097 each.  Y may not overlap an input.  Waits inside are bounded; Y is NaN where one ran out.  No context, no
+ * workspace; asynchronous on cuda_stream.  Returns as idkm_assign_groups.
  */
 int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_t ldx, const unsigned char* codes, int64_t rows, int64_t cols,
                       int64_t pitch, const void* C, int k, const void* scales, int64_t group, void* Y, int64_t ldy,
@@ -355,7 +356,8 @@ int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_t ldx, cons
  *   dz_out[row][v] = weight[row] tau (q_v - sum_{j: idx_j = v} p_j).
  * An index given twice counts twice.  A row without entries that count, or whose logits t are all -inf, has loss and gradient
  * 0.  Logits z of -inf (masked classes) have q = 0; where the teacher has p > 0 for one the loss is +inf.  A row z without a
- * finite logit has NaN.  weight (DEVICE, fp32 [rows], NULL: 1) is dL/dloss of the row.  fp32 arithmetic.
+ * finite logit has NaN.  weight (DEVICE, fp32 [rows], finite, NULL: 1) is dL/dloss of the row.  fp32 arithmetic; vocab <= 2^30, tau a
+ * normal number.  Waits inside are bounded; results are NaN where one ran out.
  *   idkm_distill_forward   writes the loss (fp32 [rows]) and, for the backward, stats_out (fp32 [rows][2], or NULL): the
  *                          logarithms of the student's and of the teacher's normaliser, in units of logits / tau;
  *   idkm_distill_backward  writes dz (rows lddz elements apart, type of z) from the same inputs and those statistics;

@@ -16,7 +16,7 @@
 // bounded; if one runs out, the blocks' results are NaN.
 //
 // What bounds it: the sums, whose loads from tensor memory compete with the products' own accumulators for it (without them 198 us
-// of 237, groups of 128; with groups of 32, four times as many, they take twice the products' time), then the products.
+// of 237, groups of 128), then the products.
 // Measured, 2048 rows through 8192 x 8192 bf16: 237 us, 1160 TFLOP/s, 0.70 of a plain library product's rate in a burst.
 #include <cuda.h>
 #include <cuda_runtime.h>
