@@ -21,7 +21,12 @@ struct CodesParams {
 };
 
 // Products for many rows of 16-bit X, on the tensor cores (idkm_codes_prompt.cu).
-cudaError_t codes_prompt(const CodesParams& p, int type, int sms, cudaStream_t st);
+struct PromptPlan {
+  int hn, split;   // half the rows of X of a tile; pairs of blocks that share its columns
+  long long ns;    // what it takes, about
+};
+PromptPlan codes_prompt_plan(const CodesParams& p, int sms);
+cudaError_t codes_prompt(const CodesParams& p, int type, const PromptPlan& plan, int sms, cudaStream_t st);
 
 __device__ __forceinline__ float code_scale(unsigned short u, __nv_bfloat16*) { return __uint_as_float((unsigned)u << 16); }
 __device__ __forceinline__ float code_scale(unsigned short u, __half*) { return __half2float(__ushort_as_half(u)); }

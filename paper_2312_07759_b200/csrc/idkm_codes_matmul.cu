@@ -574,8 +574,19 @@ cudaError_t few_launch(const CodesParams& p, int sms, cudaStream_t st) {
   f.per_block = tiles / blocks;
   f.extra = tiles % blocks;
   const bool parts = f.kept > 0;
-  return p.tokens <= 8 ? (parts ? few_launch<T, Q, 1, SCALED, true>(p, f, blocks, st) : few_launch<T, Q, 1, SCALED, false>(p, f, blocks, st))
-                       : (parts ? few_launch<T, Q, 2, SCALED, true>(p, f, blocks, st) : few_launch<T, Q, 2, SCALED, false>(p, f, blocks, st));
+  if (p.tokens > 8) {
+    // X in parts is slow for so many rows (the parts are short, a batch is a tile): about 350 ns a tile of rows and a chunk.  The tensor cores
+    // of pairs of blocks take less for large W: 16 rows through 8192 x 28672, groups of 128, 143 us and 71; 9 through 4096 x 14336, groups of
+    // 64, 33 and 52; 14 through 535 x 11392, groups of 32, 28 and 39.
+    if (parts) {
+      const PromptPlan plan = codes_prompt_plan(p, sms);
+      if (plan.ns < 350ll * ((tiles + blocks - 1) / blocks) * ((p.cols + FEW_CHUNK - 1) / FEW_CHUNK))
+        return codes_prompt(p, std::is_same<T, __half>::value ? ELEM_F16 : ELEM_BF16, plan, sms, st);
+      return few_launch<T, Q, 2, SCALED, true>(p, f, blocks, st);
+    }
+    return few_launch<T, Q, 2, SCALED, false>(p, f, blocks, st);
+  }
+  return parts ? few_launch<T, Q, 1, SCALED, true>(p, f, blocks, st) : few_launch<T, Q, 1, SCALED, false>(p, f, blocks, st);
 }
 
 template <class T>
@@ -641,6 +652,6 @@ extern "C" int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   if (type == ELEM_F32) return rows_launch(p, sms, st) == cudaSuccess ? IDKM_OK : IDKM_ERR_CUDA;
   const bool few = tokens <= FEW_TOKENS;
-  const cudaError_t rc = !few ? codes_prompt(p, type, sms, st) : type == ELEM_BF16 ? few_launch<__nv_bfloat16>(p, sms, st) : few_launch<__half>(p, sms, st);
+  const cudaError_t rc = !few ? codes_prompt(p, type, codes_prompt_plan(p, sms), sms, st) : type == ELEM_BF16 ? few_launch<__nv_bfloat16>(p, sms, st) : few_launch<__half>(p, sms, st);
   return rc == cudaSuccess ? IDKM_OK : IDKM_ERR_CUDA;
 }

@@ -15,12 +15,16 @@
 // that have been added -- is counted in the first block's barriers, by both; what it frees it tells both.  Every wait is
 // bounded; if one runs out, the blocks' results are NaN.
 //
+// Where there are fewer tiles than pairs of blocks, 2 or 4 pairs of a cluster share a tile's columns; their sums meet in the first one's
+// shared memory, in a fixed order (32 rows of X through 8192 x 28672: 129 us -> 71 with 2 pairs; 40 through 535 x 11392: 54 -> 22 with 4).
+//
 // What bounds it: the sums, whose loads from tensor memory compete with the products' own accumulators for it (without them 198 us
 // of 237, groups of 128), then the products.
 // Measured, 2048 rows through 8192 x 8192 bf16: 237 us, 1160 TFLOP/s, 0.70 of a plain library product's rate in a burst.
 #include <cuda.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
+#include <atomic>
 #include <type_traits>
 #include "idkm_codes.cuh"
 #include "idkm_per_device.h"
@@ -31,6 +35,7 @@ namespace {
 
 constexpr int PR_M = 128, PR_BLOCK = 768, PR_K = 128;   // rows of W of a tile, threads, columns of a chunk (one buffer of the first operand)
 constexpr int PR_XS = 6, PR_CS = 3, PR_DS = 3;          // stages of X (64 columns), of codes (256 columns), accumulators
+constexpr int PR_SPLIT = 4;                             // pairs of blocks that share a tile's columns, at most
 // shared memory: the codes before the table, which lies on a multiple of 64 KB (an address is put together by bytes), X after it
 constexpr int PR_TABLE = 64 * 1024, PR_CODES = PR_M * 128, PR_FRONT = PR_TABLE - 1024;   // (shared memory starts at 1 KB or above)
 
@@ -39,6 +44,7 @@ struct PrCfg {
   static constexpr int N = 2 * HN, X_HALF = HN / 2 * 128, X_STAGE = 2 * X_HALF;   // a block's rows of X for either accumulator
   static constexpr int SMEM = PR_FRONT + PR_TABLE + PR_XS * X_STAGE;
   static_assert(SMEM + 1024 + 256 <= 228 * 1024 && PR_CS * PR_CODES + 8192 <= PR_TABLE, "the X stages after the table, the codes' before");
+  static_assert(1024 * HN <= PR_TABLE + PR_XS * X_STAGE, "the sums of a block fit there");
   static constexpr int A0 = PR_DS * HN, COLS = A0 + 128 <= 256 ? 256 : 512;   // columns of tensor memory: accumulators, then two buffers of 64
 };
 
@@ -93,9 +99,9 @@ __device__ __forceinline__ void pr_arrived(unsigned (&r)[W]) {
 #pragma unroll
   for (int i = 0; i < W; ++i) asm volatile("" : "+r"(r[i]));
 }
-// to the barrier of either block, once the products issued so far are done
-__device__ __forceinline__ void pr_commit(unsigned bar) {
-  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((unsigned short)3) : "memory");
+// to the barrier of either block of the pair, once the products issued so far are done
+__device__ __forceinline__ void pr_commit(unsigned bar, unsigned short pair) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"(pair) : "memory");
 }
 __device__ __forceinline__ void pr_tma(unsigned to, const CUtensorMap* map, int x, int y, unsigned bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
@@ -106,11 +112,16 @@ __device__ __forceinline__ void pr_tma_pair(unsigned to, const CUtensorMap* map,
   asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                ::"r"(to), "l"(map), "r"(x), "r"(y), "r"(first_bar) : "memory");
 }
-// the first block's barrier
-__device__ __forceinline__ unsigned pr_first(unsigned bar) {
+// an address of a block of the cluster
+__device__ __forceinline__ unsigned pr_there(unsigned at, unsigned block) {
   unsigned r;
-  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(bar));
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(at), "r"(block));
   return r;
+}
+// all threads of the cluster
+__device__ __forceinline__ void pr_meet() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // (What is handed over lies in tensor memory, and the fence before orders it: nothing written to memory has to be waited for.)
 __device__ __forceinline__ void pr_arrive_first(unsigned first_bar) {
@@ -148,7 +159,7 @@ struct PrRing {
 // SEGS: groups of a chunk (1 where groups are longer), whose sums are taken one by one.
 template <class T, int HN, int SEGS, bool TMA>
 __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_constant__ CodesParams p, const __grid_constant__ CUtensorMap map_codes,
-                                                                 const __grid_constant__ CUtensorMap map_x) {
+                                                                 const __grid_constant__ CUtensorMap map_x, int split) {
   using Cfg = PrCfg<HN>;
   constexpr int STEPS = 8 / SEGS;   // products of 16 columns of a segment
   T* const type = nullptr;
@@ -160,6 +171,8 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
   const unsigned codes0 = base - PR_CS * PR_CODES, x0_at = base + PR_TABLE;
   unsigned char* const mem_x = pr_raw + (x0_at - raw);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, rank = blockIdx.x & 1;
+  const int pair = (int)(blockIdx.x % (unsigned)(2 * split)) >> 1;   // of the cluster
+  const unsigned first = 2u * (unsigned)pair;
   const unsigned bars = pr_smem(s_bar);
   const unsigned x_full = bars, x_empty = x_full + 8 * PR_XS, c_full = x_empty + 8 * PR_XS, c_empty = c_full + 8 * PR_CS;
   const unsigned a_full = c_empty + 8 * PR_CS, a_empty = a_full + 16, d_full = a_empty + 16, d_empty = d_full + 8 * PR_DS;
@@ -195,15 +208,15 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  // (both blocks run, their barriers are ready)
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  pr_meet();   // (all blocks run, their barriers are ready)
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const unsigned tmem = *reinterpret_cast<volatile unsigned*>(&s_tmem);
 
-  const int n_chunks = (int)((p.cols + PR_K - 1) / PR_K);
+  // this pair's chunks: from chunk0 on (an even one, codes are copied by two)
+  const int all_chunks = (int)((p.cols + PR_K - 1) / PR_K), share = ((all_chunks + 1) / 2 + split - 1) / split * 2, chunk0 = min(pair * share, all_chunks);
+  const int n_chunks = min(share, all_chunks - chunk0);
   const long long tiles_x = (p.tokens + Cfg::N - 1) / Cfg::N, tiles = tiles_x * ((p.rows + 2 * PR_M - 1) / (2 * PR_M));
-  const long long tile0 = blockIdx.x >> 1, tile_on = gridDim.x >> 1;
+  const long long tile0 = blockIdx.x / (unsigned)(2 * split), tile_on = gridDim.x / (unsigned)(2 * split);
   bool ok = true;
 
   if (warp < 16) {   // ---- the sums
@@ -212,7 +225,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
     const int h = warp >> 3, part = warp >> 2 & 1, quad = warp & 3;
     const unsigned from0 = tmem + ((unsigned)(quad * 32) << 16) + (unsigned)(part * HC);
     const int per = SEGS > 1 ? 1 : (int)(p.group / PR_K);   // chunks of a group
-    const unsigned d_added = pr_first(d_empty);
+    const unsigned d_added = pr_there(d_empty, first);
     int buffer = h;        // every second accumulation is this half's, the accumulators take turns
     unsigned parity = 0;
     for (long long tile = tile0; tile < tiles; tile += tile_on) {
@@ -221,8 +234,8 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
       float acc[HC];
 #pragma unroll
       for (int i = 0; i < HC; ++i) acc[i] = 0.f;
-      int g = 0, left = per;   // the group, and chunks of it that are left
-      unsigned short next = s_row ? __ldg(s_row) : (unsigned short)0;
+      int g = SEGS > 1 ? chunk0 * SEGS : chunk0 / per, left = SEGS > 1 ? per : per - (chunk0 - g * per);   // the group, and chunks of it that are left
+      unsigned short next = s_row && g < p.n_groups ? __ldg(s_row + g) : (unsigned short)0;
 #pragma unroll 1
       for (int seg = 0; seg < n_chunks * SEGS; ++seg) {
         const float s = p.scales ? code_scale(next, type) : 1.f;
@@ -264,7 +277,27 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
           if (at + W < HC) add(r1, at + W);
         }
       }
-      if (row < p.rows) {
+      // the pairs' sums: a half of the pairs sends, through the table's memory and that of X behind it, the other half adds
+      for (int step = 1; step < split; step *= 2) {
+        __syncwarp();
+        pr_meet();   // (the table and X are not needed any more, what was sent before has been read)
+        if (pair % (2 * step) == step) {
+          const unsigned there = pr_there(base, (unsigned)(2 * (pair - step) + rank)) + (unsigned)tid * 4u;
+#pragma unroll
+          for (int i = 0; i < HC; ++i)
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(there + (unsigned)i * 2048u), "f"(ok ? acc[i] : __int_as_float(0x7fc00000)) : "memory");
+        }
+        pr_meet();
+        if (pair % (2 * step) == 0) {
+#pragma unroll
+          for (int i = 0; i < HC; ++i) {
+            float v;
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(base + (unsigned)tid * 4u + (unsigned)i * 2048u) : "memory");
+            acc[i] += v;
+          }
+        }
+      }
+      if (row < p.rows && pair == 0) {
         T* y = reinterpret_cast<T*>(p.Y) + row;
 #pragma unroll
         for (int i = 0; i < HC; ++i)
@@ -278,7 +311,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
     asm volatile("or.b32 %0, %1, %2;" : "=r"(mine) : "r"(base), "r"((unsigned)lane * 4u) : "memory");
     const unsigned my_codes = codes0 + (unsigned)r * 128u;
     const unsigned to = tmem + ((unsigned)(quad * 32) << 16) + (unsigned)Cfg::A0;
-    const unsigned a_there = pr_first(a_full);
+    const unsigned a_there = pr_there(a_full, first);
     PrRing<PR_CS> cr;
     PrRing<2> ar;
     for (long long tile = tile0; tile < tiles; tile += tile_on) {
@@ -325,6 +358,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
         const unsigned kind = std::is_same<T, __half>::value ? 0u : 1u;
         const unsigned idesc = (1u << 4) | (kind << 7) | (kind << 10) | ((unsigned)(HN >> 3) << 17) | ((unsigned)(2 * PR_M >> 4) << 24);
         const unsigned d0 = __shfl_sync(0xffffffffu, tmem, 0), x_base = (x0_at >> 4) | (1u << 16);
+        const unsigned short both = (unsigned short)(3u << first);
         PrRing<PR_XS> xr;
         PrRing<2> ar;
         PrRing<PR_DS> dr;
@@ -353,11 +387,11 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
                     const int k16 = seg * STEPS + i;
                     pr_mma(d0 + (unsigned)(dr.at * HN), a0 + (unsigned)(k16 * 8), (k16 < 4 ? b0 : b1) + (unsigned)(h * (Cfg::X_HALF / 16) + (k16 & 3) * 2), idesc, i > 0);
                   }
-                  pr_commit(d_full + 8 * dr.at);
+                  pr_commit(d_full + 8 * dr.at, both);
                   if (seg + 1 == SEGS && h == 1) {
-                    pr_commit(a_empty + 8 * ar.at);
-                    pr_commit(x_empty + 8 * x0);
-                    pr_commit(x_empty + 8 * x1);
+                    pr_commit(a_empty + 8 * ar.at, both);
+                    pr_commit(x_empty + 8 * x0, both);
+                    pr_commit(x_empty + 8 * x1, both);
                   }
                 }
                 __syncwarp();
@@ -372,7 +406,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
       PrRing<PR_XS> xr;
       PrRing<PR_CS> cr;
       bool x_filled = false, c_filled = false;   // every stage has been filled once
-      const unsigned x_there = pr_first(x_full);
+      const unsigned x_there = pr_there(x_full, first);
       for (long long tile = tile0; tile < tiles && ok; tile += tile_on) {
         const long long row0 = (tile / tiles_x * 2 + rank) * PR_M, tok0 = tile % tiles_x * Cfg::N;
 #pragma unroll 1
@@ -381,7 +415,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
             if (c_filled) ok = code_wait(c_empty + 8 * cr.at, cr.parity ^ 1u);
             if (ok) {
               pr_expect(c_full + 8 * cr.at, PR_CODES);
-              pr_tma(codes0 + cr.at * PR_CODES, &map_codes, c * (PR_K / 2), (int)row0, c_full + 8 * cr.at);
+              pr_tma(codes0 + cr.at * PR_CODES, &map_codes, (chunk0 + c) * (PR_K / 2), (int)row0, c_full + 8 * cr.at);
               cr.next();
               if (cr.at == 0) c_filled = true;
             }
@@ -396,7 +430,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
                   if (rank == 0) pr_expect(x_full + 8 * xr.at, 2 * Cfg::X_STAGE);   // (of both blocks)
 #pragma unroll
                   for (int h = 0; h < 2; ++h)
-                    pr_tma_pair(at + h * Cfg::X_HALF, &map_x, c * PR_K + j * 64, (int)tok0 + h * HN + rank * (HN / 2), x_there + 8 * xr.at);
+                    pr_tma_pair(at + h * Cfg::X_HALF, &map_x, (chunk0 + c) * PR_K + j * 64, (int)tok0 + h * HN + rank * (HN / 2), x_there + 8 * xr.at);
                 }
               }
             } else {
@@ -406,7 +440,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
                 const int m = i >> 3, v = i & 7, h = m >= HN / 2;   // (halves are whole groups of 8 rows: the swizzle is that of the row in either)
                 const long long tok = tok0 + h * HN + rank * (HN / 2) + (m - h * (HN / 2));
                 uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                if (tok < p.tokens) x = code_load8(reinterpret_cast<const T*>(p.X) + tok * p.ldx, c * PR_K + j * 64 + v * 8, p.cols);
+                if (tok < p.tokens) x = code_load8(reinterpret_cast<const T*>(p.X) + tok * p.ldx, (chunk0 + c) * PR_K + j * 64 + v * 8, p.cols);
                 *reinterpret_cast<uint4*>(mem_x + xr.at * Cfg::X_STAGE + m * 128 + ((v ^ (m & 7)) << 4)) = x;
               }
               asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -427,11 +461,14 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
     }
   }
   __syncwarp();
+  if (warp >= 16)
+    for (int step = 1; step < split; step *= 2) {   // (where the sums meet)
+      pr_meet();
+      pr_meet();
+    }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
-  // (neither block leaves while the other may still tell it something)
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  pr_meet();   // (no block leaves while another may still tell it something)
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   if (warp == 20) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(Cfg::COLS));
 }
@@ -457,8 +494,41 @@ bool pr_map(CUtensorMap& m, CUtensorMapDataType type, int bytes, const void* at,
                      CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+void pr_config(cudaLaunchConfig_t& cfg, cudaLaunchAttribute (&attr)[1], long long clusters, int split, int smem, cudaStream_t st) {
+  cfg.gridDim = dim3((unsigned)(2 * split * clusters));
+  cfg.blockDim = dim3(PR_BLOCK);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)(2 * split);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+}
+// Clusters of `split` pairs that run at once on the current device (on a B200 74, 33 and 15 of 1, 2 and 4 pairs: fewer than its
+// multiprocessors would make, as a cluster stays within a part of them).  Asked for once a device; a block has a multiprocessor in every variant.
+int pr_clusters(int split) {
+  static std::atomic<int> known[64][PR_SPLIT + 1];   // (0: not asked for yet)
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess) return 0;
+  const bool keep = dev >= 0 && dev < 64;
+  int n = keep ? known[dev][split].load(std::memory_order_relaxed) : 0;
+  if (n > 0) return n;
+  static PerDevice limit;
+  if (allow_smem(limit, idkm_codes_prompt<__nv_bfloat16, 16, 1, true>, PrCfg<16>::SMEM) != cudaSuccess) return 0;
+  cudaLaunchConfig_t cfg = {};
+  cudaLaunchAttribute attr[1];
+  pr_config(cfg, attr, 1, split, PrCfg<16>::SMEM, nullptr);
+  if (cudaOccupancyMaxActiveClusters(&n, idkm_codes_prompt<__nv_bfloat16, 16, 1, true>, &cfg) != cudaSuccess) {
+    (void)cudaGetLastError();
+    return 0;
+  }
+  if (keep) known[dev][split].store(n, std::memory_order_relaxed);
+  return n;
+}
+
 template <class T, int HN, int SEGS, bool TMA>
-cudaError_t pr_launch(const CodesParams& p, int sms, cudaStream_t st) {
+cudaError_t pr_launch(const CodesParams& p, int split, int sms, cudaStream_t st) {
   using Cfg = PrCfg<HN>;
   CUtensorMap codes, x = {};
   if (!pr_map(codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, p.codes, (p.cols + 31) / 32 * 16, p.rows, p.pitch, PR_M)) return cudaErrorInvalidValue;
@@ -470,46 +540,44 @@ cudaError_t pr_launch(const CodesParams& p, int sms, cudaStream_t st) {
   if (rc != cudaSuccess) return rc;
   const long long tiles = (p.rows + 2 * PR_M - 1) / (2 * PR_M) * ((p.tokens + Cfg::N - 1) / Cfg::N), pairs = sms / 2;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(2 * (tiles < pairs ? tiles : pairs)));
-  cfg.blockDim = dim3(PR_BLOCK);
-  cfg.dynamicSmemBytes = Cfg::SMEM;
-  cfg.stream = st;
   cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = 2;
-  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, idkm_codes_prompt<T, HN, SEGS, TMA>, p, codes, x);
+  pr_config(cfg, attr, split > 1 || tiles < pairs ? tiles : pairs, split, Cfg::SMEM, st);   // (shared columns: a tile for every cluster)
+  return cudaLaunchKernelEx(&cfg, idkm_codes_prompt<T, HN, SEGS, TMA>, p, codes, x, split);
 }
 
 template <class T, int HN>
-cudaError_t pr_launch(const CodesParams& p, int sms, cudaStream_t st) {
+cudaError_t pr_launch(const CodesParams& p, int split, int sms, cudaStream_t st) {
   const int segs = !p.scales || p.group >= 128 ? 1 : (int)(128 / p.group);
-  if (p.vec_x) return segs == 1 ? pr_launch<T, HN, 1, true>(p, sms, st) : segs == 2 ? pr_launch<T, HN, 2, true>(p, sms, st) : pr_launch<T, HN, 4, true>(p, sms, st);
-  return segs == 1 ? pr_launch<T, HN, 1, false>(p, sms, st) : segs == 2 ? pr_launch<T, HN, 2, false>(p, sms, st) : pr_launch<T, HN, 4, false>(p, sms, st);
+  if (p.vec_x) return segs == 1 ? pr_launch<T, HN, 1, true>(p, split, sms, st) : segs == 2 ? pr_launch<T, HN, 2, true>(p, split, sms, st) : pr_launch<T, HN, 4, true>(p, split, sms, st);
+  return segs == 1 ? pr_launch<T, HN, 1, false>(p, split, sms, st) : segs == 2 ? pr_launch<T, HN, 2, false>(p, split, sms, st) : pr_launch<T, HN, 4, false>(p, split, sms, st);
 }
 
 }  // namespace
 
-cudaError_t codes_prompt(const CodesParams& p, int type, int sms, cudaStream_t st) {
-  if (!pr_encode()) return cudaErrorNotSupported;
-  if (p.rows > INT32_MAX - PR_M || p.cols > INT32_MAX - 512 || p.tokens > INT32_MAX - 256) return cudaErrorInvalidValue;
+PromptPlan codes_prompt_plan(const CodesParams& p, int sms) {
   // rows of X of a tile: those whose waves of tiles cost least.  A chunk of 128 columns took 0.63, 0.66, 0.76 and 0.92 us at HN =
   // 16, 32, 64 and 128 (2048 rows through 8192 x 8192: 1120, 594, 342 and 237 us in all), about 1200 + 5 HN halves of a nanosecond.
-  const long long tiles_w = (p.rows + 2 * PR_M - 1) / (2 * PR_M), pairs = sms / 2;
-  int best = 128;
-  long long least = INT64_MAX;
-  for (int hn = 16; hn <= 128; hn *= 2) {
-    const long long tiles = tiles_w * ((p.tokens + 2 * hn - 1) / (2 * hn)), cost = (tiles + pairs - 1) / pairs * (1200 + 5 * hn);
-    if (cost < least || (cost == least && hn <= best)) {
-      least = cost;
-      best = hn;
+  // Where there are few tiles, the pairs of a cluster share a tile's columns; sums that meet cost about 1000 + 20 HN ns a step.
+  const long long tiles_w = (p.rows + 2 * PR_M - 1) / (2 * PR_M), pairs = sms / 2, chunks = (p.cols + PR_K - 1) / PR_K;
+  PromptPlan plan = {128, 1, INT64_MAX};
+  for (int hn = 16; hn <= 128; hn *= 2)
+    for (int s = 1, steps = 0; s <= PR_SPLIT; s *= 2, ++steps) {
+      const long long tiles = tiles_w * ((p.tokens + 2 * hn - 1) / (2 * hn));
+      if (s > 1 && (tiles * s > pairs || chunks < 4 * s || tiles > pr_clusters(s))) break;
+      const long long cost = (s > 1 ? 1 : (tiles + pairs - 1) / pairs) * ((chunks + s - 1) / s) * (1200 + 5 * hn) + steps * (2000 + 40 * hn);
+      if (cost < plan.ns) plan = {hn, s, cost};
     }
-  }
+  // (groups of 64 and 32: 17 rows through 4096 x 14336 39 and 52 us, 14 through 535 x 11392 22 and 39)
+  const int segments = !p.scales || p.group >= 128 ? 10 : p.group == 64 ? 14 : 18;
+  plan.ns = plan.ns / 20 * segments;
+  return plan;
+}
+
+cudaError_t codes_prompt(const CodesParams& p, int type, const PromptPlan& plan, int sms, cudaStream_t st) {
+  if (!pr_encode()) return cudaErrorNotSupported;
   auto run = [&](auto* t) {
     using T = std::remove_pointer_t<decltype(t)>;
-    return best == 16 ? pr_launch<T, 16>(p, sms, st) : best == 32 ? pr_launch<T, 32>(p, sms, st) : best == 64 ? pr_launch<T, 64>(p, sms, st) : pr_launch<T, 128>(p, sms, st);
+    return plan.hn == 16 ? pr_launch<T, 16>(p, plan.split, sms, st) : plan.hn == 32 ? pr_launch<T, 32>(p, plan.split, sms, st) : plan.hn == 64 ? pr_launch<T, 64>(p, plan.split, sms, st) : pr_launch<T, 128>(p, plan.split, sms, st);
   };
   return type == ELEM_BF16 ? run((__nv_bfloat16*)nullptr) : run((__half*)nullptr);
 }

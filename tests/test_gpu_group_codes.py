@@ -422,3 +422,17 @@ def test_products_whose_columns_come_in_parts(t, tokens, rows, cols, group):
     ref = B.matmul_codes(X, codes, C, s, group)
     _check_product(torch, ref, X, codes, C, s, group)
     assert torch.equal(B.matmul_codes(X, codes, C, s, group), ref)
+
+
+@pytest.mark.parametrize("t", ["bfloat16", "float16"])
+@pytest.mark.parametrize("group", [0, 32, 64, 128, 384, 1280])
+@pytest.mark.parametrize("tokens,rows,cols", [(17, 300, 4099), (40, 535, 11392), (64, 257, 1000), (100, 2048, 1160), (130, 200, 2312), (300, 700, 5128), (513, 256, 3200)])
+def test_products_whose_columns_are_shared(t, group, tokens, rows, cols):
+    """Few tiles, whose columns several pairs of blocks share: shares that begin within a group, that are shorter than others or empty."""
+    import torch
+    from paper_2312_07759_b200 import binding as B
+    X, codes, C, s = _case(torch, tokens, rows, cols, group, t)
+    ref = B.matmul_codes(X, codes, C, s, group)
+    _check_product(torch, ref, X, codes, C, s, group)
+    for _ in range(3):
+        assert torch.equal(B.matmul_codes(X, codes, C, s, group), ref)
