@@ -48,17 +48,13 @@ __device__ __forceinline__ uint4 code_align8(const uint4& a, const uint4& b, uns
   }
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-// Eight 16-bit elements of a row from column k on, zeros past its end, whatever the row's alignment: from the one or two
-// 16-byte words that hold them.  (A word that holds one byte of the row lies in the row's pages.)
-__device__ __forceinline__ uint4 code_load8(const void* row, long long k, long long cols) {
-  uint4 a = make_uint4(0u, 0u, 0u, 0u), b = a;
-  if (k >= cols) return a;
-  const uintptr_t at = (uintptr_t)row + 2 * k, end = (uintptr_t)row + 2 * cols;
-  const uint4* word = reinterpret_cast<const uint4*>(at & ~(uintptr_t)15);
-  const unsigned off = (unsigned)(at & 15u);
-  a = __ldg(word);
-  if (off && (uintptr_t)(word + 1) < end) b = __ldg(word + 1);
-  return code_align8(a, b, off, cols - k < 8 ? (int)(cols - k) : 8);
+// The 16-byte word of memory at `word` and the next one, each where it is wanted, zeros elsewhere; nothing branches, so that what
+// is asked for next does not wait.
+__device__ __forceinline__ void code_ask(uint4& a, uint4& b, uintptr_t word, int first, int second) {
+  a = b = make_uint4(0u, 0u, 0u, 0u);
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %9, 0;\n\tsetp.ne.b32 q, %10, 0;\n\t@p ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%8];\n\t"
+               "@q ld.global.nc.v4.u32 {%4, %5, %6, %7}, [%8+16];\n\t}"
+               : "+r"(a.x), "+r"(a.y), "+r"(a.z), "+r"(a.w), "+r"(b.x), "+r"(b.y), "+r"(b.z), "+r"(b.w) : "l"(word), "r"(first), "r"(second));
 }
 
 constexpr int CODE_POLLS = 1 << 22;   // (each waits for some time itself)

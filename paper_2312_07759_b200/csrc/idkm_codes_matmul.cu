@@ -309,10 +309,7 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
     const uintptr_t row = (uintptr_t)(X + m * p.ldx), at = row + 2 * k, end = row + 2 * p.cols;
     const uintptr_t word = at & ~(uintptr_t)15;
     const int first = i < n_words && at < end, second = first && (at & 15) && word + 16 < end;
-    a = b = make_uint4(0u, 0u, 0u, 0u);
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %9, 0;\n\tsetp.ne.b32 q, %10, 0;\n\t@p ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%8];\n\t"
-                 "@q ld.global.nc.v4.u32 {%4, %5, %6, %7}, [%8+16];\n\t}"
-                 : "+r"(a.x), "+r"(a.y), "+r"(a.z), "+r"(a.w), "+r"(b.x), "+r"(b.y), "+r"(b.z), "+r"(b.w) : "l"(word), "r"(first), "r"(second));
+    code_ask(a, b, word, first, second);
   };
   auto place = [&](int i, int col0, const uint4& a, const uint4& b) {
     if (i >= n_words) return;

@@ -35,6 +35,7 @@ namespace {
 
 constexpr int PR_M = 128, PR_BLOCK = 768, PR_K = 128;   // rows of W of a tile, threads, columns of a chunk (one buffer of the first operand)
 constexpr int PR_XS = 6, PR_CS = 3, PR_DS = 3;          // stages of X (64 columns), of codes (256 columns), accumulators
+constexpr int PR_ASK = 2;                               // words of X that a thread has under way where TMA cannot copy it
 constexpr int PR_SPLIT = 4;                             // pairs of blocks that share a tile's columns, at most
 // shared memory: the codes before the table, which lies on a multiple of 64 KB (an address is put together by bytes), X after it
 constexpr int PR_TABLE = 64 * 1024, PR_CODES = PR_M * 128, PR_FRONT = PR_TABLE - 1024;   // (shared memory starts at 1 KB or above)
@@ -426,12 +427,29 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
             } else {
               if (x_filled && ok) ok = code_wait(x_empty + 8 * xr.at, xr.parity ^ 1u);
               ok = __all_sync(0xffffffffu, ok);   // (warps stay together whatever comes of it)
-              for (int i = tid - 21 * 32; i < HN * 8; i += 96) {
-                const int m = i >> 3, v = i & 7, h = m >= HN / 2;   // (halves are whole groups of 8 rows: the swizzle is that of the row in either)
-                const long long tok = tok0 + h * HN + rank * (HN / 2) + (m - h * (HN / 2));
-                uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                if (tok < p.tokens) x = code_load8(reinterpret_cast<const T*>(p.X) + tok * p.ldx, (chunk0 + c) * PR_K + j * 64 + v * 8, p.cols);
-                *reinterpret_cast<uint4*>(mem_x + xr.at * Cfg::X_STAGE + m * 128 + ((v ^ (m & 7)) << 4)) = x;
+              // (what PR_ASK words need is asked for before the first is looked at)
+              for (int i0 = tid - 21 * 32; i0 < HN * 8; i0 += 96 * PR_ASK) {
+                uint4 a[PR_ASK], b[PR_ASK];
+                const int k = (chunk0 + c) * PR_K + j * 64 + (i0 & 7) * 8;   // (96 is a multiple of 8: of all of them)
+                auto row_of = [&](int i) {
+                  const int m = i >> 3, h = m >= HN / 2;   // (halves are whole groups of 8 rows: the swizzle is that of the row in either)
+                  return tok0 + h * HN + rank * (HN / 2) + (m - h * (HN / 2));
+                };
+#pragma unroll
+                for (int u = 0; u < PR_ASK; ++u) {
+                  const int i = i0 + u * 96;
+                  const long long tok = row_of(i);
+                  const uintptr_t row = (uintptr_t)(reinterpret_cast<const T*>(p.X) + tok * p.ldx), at = row + 2ll * k, end = row + 2 * p.cols, word = at & ~(uintptr_t)15;
+                  const int one = i < HN * 8 && tok < p.tokens && at < end, two = one && (at & 15) && word + 16 < end;
+                  code_ask(a[u], b[u], word, one, two);
+                }
+#pragma unroll
+                for (int u = 0; u < PR_ASK; ++u) {
+                  const int i = i0 + u * 96, m = i >> 3;
+                  if (i >= HN * 8) break;
+                  const unsigned off = (unsigned)((uintptr_t)(reinterpret_cast<const T*>(p.X) + row_of(i) * p.ldx) & 15u);   // (columns by eights: the row's)
+                  *reinterpret_cast<uint4*>(mem_x + xr.at * Cfg::X_STAGE + m * 128 + (((i & 7) ^ (m & 7)) << 4)) = code_align8(a[u], b[u], off, (int)p.cols - k);
+                }
               }
               asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
               __syncwarp();
