@@ -63,19 +63,23 @@ __global__ void __launch_bounds__(ROWS_BLOCK) idkm_codes_rows(const __grid_const
         // X is asked for before anything is looked at; rows past the last one count for nothing
         float xs[TOK][ROWS_LANE];
         if (whole) {
+          float4 v[TOK][ROWS_LANE / 4];
           const float* x = X + c;
 #pragma unroll
           for (int m = 0; m < TOK; ++m) {
 #pragma unroll
-            for (int q = 0; q < ROWS_LANE / 4; ++q) {
-              const float4 v = __ldg(reinterpret_cast<const float4*>(x) + q);
-              xs[m][4 * q] = v.x;
-              xs[m][4 * q + 1] = v.y;
-              xs[m][4 * q + 2] = v.z;
-              xs[m][4 * q + 3] = v.w;
-            }
+            for (int q = 0; q < ROWS_LANE / 4; ++q) v[m][q] = __ldg(reinterpret_cast<const float4*>(x) + q);
             if (m + 1 < n_tok) x += p.ldx;   // (rows past the last one: the last)
           }
+#pragma unroll
+          for (int m = 0; m < TOK; ++m)
+#pragma unroll
+            for (int q = 0; q < ROWS_LANE / 4; ++q) {
+              xs[m][4 * q] = v[m][q].x;
+              xs[m][4 * q + 1] = v[m][q].y;
+              xs[m][4 * q + 2] = v[m][q].z;
+              xs[m][4 * q + 3] = v[m][q].w;
+            }
         } else {
 #pragma unroll
           for (int m = 0; m < TOK; ++m)
