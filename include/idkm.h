@@ -334,7 +334,7 @@ int64_t idkm_group_codes_pitch(int64_t cols);   /* 16 ceil(cols / 32); 0 for col
  * the bytes of a row up to there are read, codes past the last column count for nothing).  scales = NULL: all 1 (the codes of
  * idkm_assign for a layer of 5 <= k <= 16 scalar centroids and rows of a multiple of 32 weights).  Products and sums are in
  * fp32, the scale multiplies the fp32 sum of its group, and Y is rounded once; the order of the sums depends on the shape
- * alone.  C must be finite; a code that names no entry stands for 0.  codes 16-byte aligned, the others to their elements
+ * and the GPU alone.  C must be finite; a code that names no entry stands for 0.  codes 16-byte aligned, the others to their elements
  * (X is read fastest from 16-byte-aligned rows).  group as above, or any number >= cols: one scale a row.  Tokens, rows and columns
  * up to 2^31 - 4097 each.  Y may not overlap an input.  Waits inside are bounded; Y is NaN where one ran out.  No context, no
  * workspace; asynchronous on cuda_stream.  Returns as idkm_assign_groups.
