@@ -569,11 +569,12 @@ __global__ void __launch_bounds__(DISTILL_GRAD_BLOCK) idkm_distill_grad(const __
   __syncthreads();
   if (mine) distill_enter(s_table, at, &s_twice);
   __syncthreads();   // (every thread has read its entry's place: what follows may write it)
-  // x = z / tau - L in units of log2, for fp32 with the low parts of log2(e) / tau and of L log2(e)
+  // x = z / tau - L in units of log2, for fp32 with the low parts of log2(e) / tau and of L log2(e), which have either sign: where x is
+  // -inf already (z is, or leaves the range) they are left out
   const float lh = L * LOG2E, ll = __fmaf_rn(L, LOG2E_LOW, __fmaf_rn(L, LOG2E, -lh));
   auto q_of = [&](float z) {
     float y = __fmaf_rn(z, p.c2, -lh);
-    if (sizeof(T) == 4) y += __fmaf_rn(z, p.c2_low, -ll);
+    if (sizeof(T) == 4) y = y == none ? y : y + __fmaf_rn(z, p.c2_low, -ll);
     return w * distill_ex2(y > 0.f ? 0.f : y);   // (q <= 1, also where the rounding of a huge L says otherwise)
   };
   // (the teacher's probabilities are exp(t / tau - lse_t): as exp((t - tm) / tau) with tm = lse_t tau)
