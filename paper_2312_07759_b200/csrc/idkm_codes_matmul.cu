@@ -309,8 +309,8 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
   const int words = slab * (FEW_CHUNK / 8), n_words = tokens * words;
   auto column_of = [&](int v) { return (v >> 4) * 128 + 8 * few_column<Q>((v >> 2) & 3, v & 3); };   // place 4 q + t of a strip: for word q of thread t
   auto ask = [&](int i, int col0, uint4& a, uint4& b) {
-    const int m = (int)__umulhi((unsigned)i, f.x_words), k = col0 + column_of(i - m * words);
-    const uintptr_t row = (uintptr_t)(X + m * p.ldx), at = row + 2 * k, end = row + 2 * p.cols;
+    const int m = (int)__umulhi((unsigned)i, f.x_words), k = column_of(i - m * words);   // (columns in bytes pass 32 bits)
+    const uintptr_t row = (uintptr_t)(X + m * p.ldx), at = row + 2ll * col0 + 2 * k, end = row + 2 * p.cols;
     const uintptr_t word = at & ~(uintptr_t)15;
     const int first = i < n_words && at < end, second = first && (at & 15) && word + 16 < end;
     code_ask(a, b, word, first, second);
