@@ -107,6 +107,8 @@ lib.idkm_assign_groups.restype = C.c_int
 lib.idkm_matmul_codes.argtypes = [_vp, C.c_int, C.c_int64, C.c_int64, _vp, C.c_int64, C.c_int64, C.c_int64, _vp, C.c_int, _vp, C.c_int64,
                                   _vp, C.c_int64, _vp]
 lib.idkm_matmul_codes.restype = C.c_int
+lib.idkm_set_codes_test_hooks.argtypes = [C.c_int]
+lib.idkm_set_codes_test_hooks.restype = C.c_int
 _logits = [_vp, C.c_int, C.c_int64, C.c_int64, C.c_int64, _vp, C.c_int, _vp, C.c_int, C.c_int, C.c_float]
 lib.idkm_distill_forward.argtypes = _logits + [_vp, _vp, _vp]
 lib.idkm_distill_forward.restype = C.c_int
@@ -321,6 +323,11 @@ def matmul_codes(X, codes, Cm, scales=None, group: int = 0, out=None, stream=Non
     if rc:
         raise IdkmError(rc)
     return Y
+
+
+def set_codes_test_hooks(missing_copy: int = 0) -> None:
+    """``idkm_set_codes_test_hooks`` (host-side fault injection for ``matmul_codes``; 0 restores production behaviour)."""
+    _check(lib.idkm_set_codes_test_hooks(missing_copy))
 
 
 def _distill_inputs(z, idx, t, tau):

@@ -18,6 +18,7 @@ struct CodesParams {
   void* Y;
   long long ldy;
   int vec_x;   // rows of X start on 16-byte boundaries
+  int missing;   // of many rows of X: the chunk from which codes are not copied (a test's; below 0: none)
 };
 
 // Products for many rows of 16-bit X, on the tensor cores (idkm_codes_prompt.cu).
@@ -57,7 +58,7 @@ __device__ __forceinline__ void code_ask(uint4& a, uint4& b, uintptr_t word, int
                : "+r"(a.x), "+r"(a.y), "+r"(a.z), "+r"(a.w), "+r"(b.x), "+r"(b.y), "+r"(b.z), "+r"(b.w) : "l"(word), "r"(first), "r"(second));
 }
 
-constexpr int CODE_POLLS = 1 << 22;   // (each waits for some time itself)
+constexpr int CODE_POLLS = 1 << 19;   // (each waits for some time itself, 2 us: about a second)
 __device__ __forceinline__ bool code_wait(unsigned bar, unsigned parity) {
   for (int i = 0; i < CODE_POLLS; ++i) {
     unsigned done;

@@ -2,6 +2,7 @@
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
+#include <atomic>
 #include <type_traits>
 #include "idkm_per_device.h"
 #include "idkm_codes.cuh"
@@ -625,7 +626,15 @@ cudaError_t rows_launch(const CodesParams& p, int sms, cudaStream_t st) {
   return cudaSuccess;
 }
 
+std::atomic<int> hook_missing_copy{0};   // idkm_set_codes_test_hooks; 0 at rest
+
 }  // namespace
+
+extern "C" int idkm_set_codes_test_hooks(int missing_copy) {
+  if (missing_copy < 0 || missing_copy > (1 << 24)) return IDKM_ERR_PARAM;
+  hook_missing_copy.store(missing_copy, std::memory_order_relaxed);
+  return IDKM_OK;
+}
 
 extern "C" int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_t ldx, const unsigned char* codes, int64_t rows, int64_t cols,
                                  int64_t pitch, const void* C, int k, const void* scales, int64_t group, void* Y, int64_t ldy,
@@ -650,6 +659,7 @@ extern "C" int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_
   p.n_groups = (cols + p.group - 1) / p.group;
   p.Y = Y; p.ldy = ldy;
   p.vec_x = (uintptr_t)X % 16 == 0 && ldx * tb % 16 == 0;
+  p.missing = 2 * hook_missing_copy.load(std::memory_order_relaxed) - 2;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   if (type == ELEM_F32) return rows_launch(p, sms, st) == cudaSuccess ? IDKM_OK : IDKM_ERR_CUDA;
   const bool few = tokens <= FEW_TOKENS;

@@ -13,7 +13,8 @@
 // Roles (24 warps a block): 0-15 sums, 16-19 lookups, 20 issues the products (the first block's, for both), 21 and 22 the copies
 // (TMA; X whose rows do not start on 16 bytes is copied by warps 21-23).  What the issuing thread waits for -- X, lookups, accumulators
 // that have been added -- is counted in the first block's barriers, by both; what it frees it tells both.  Every wait is
-// bounded; if one runs out, the blocks' results are NaN.
+// bounded.  Whoever's wait runs out hands nothing over any more, so that the waits for it run out too, those of the sums last, and the
+// pair's results are NaN.
 //
 // Where there are fewer tiles than pairs of blocks, 2 or 4 pairs of a cluster share a tile's columns; their sums meet in the first one's
 // shared memory, in a fixed order (32 rows of X through 8192 x 28672: 129 us -> 71 with 2 pairs; 40 through 535 x 11392: 54 -> 22 with 4).
@@ -145,6 +146,11 @@ struct PrRing {
       parity ^= 1u;
     }
   }
+  // Waits for what each buffer was last begun with (a buffer that was never begun with: not at all).
+  __device__ __forceinline__ void drain(unsigned full) const {
+#pragma unroll 1
+    for (int i = 0; i < S; ++i) code_wait(full + 8 * i, i < at ? parity : parity ^ 1u);
+  }
 };
 
 // SEGS: groups of a chunk (1 where groups are longer), whose sums are taken one by one.
@@ -155,7 +161,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
   constexpr int STEPS = 8 / SEGS;   // products of 16 columns of a segment
   T* const type = nullptr;
   extern __shared__ __align__(16) unsigned char pr_raw[];
-  __shared__ __align__(8) unsigned long long s_bar[2 * PR_XS + 2 * PR_CS + 4 + 2 * PR_DS];
+  __shared__ __align__(8) unsigned long long s_bar[2 * PR_XS + 2 * PR_CS + 4 + 2 * PR_DS + 1];
   __shared__ unsigned s_tmem;
   const unsigned raw = pr_smem(pr_raw), base = (raw + PR_TABLE - 1) & ~(unsigned)(PR_TABLE - 1);
   // (codes and X on multiples of 1024, which the swizzle goes by)
@@ -166,7 +172,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
   const unsigned first = 2u * (unsigned)pair;
   const unsigned bars = pr_smem(s_bar);
   const unsigned x_full = bars, x_empty = x_full + 8 * PR_XS, c_full = x_empty + 8 * PR_XS, c_empty = c_full + 8 * PR_CS;
-  const unsigned a_full = c_empty + 8 * PR_CS, a_empty = a_full + 16, d_full = a_empty + 16, d_empty = d_full + 8 * PR_DS;
+  const unsigned a_full = c_empty + 8 * PR_CS, a_empty = a_full + 16, d_full = a_empty + 16, d_empty = d_full + 8 * PR_DS, all_done = d_empty + 8 * PR_DS;
   if (tid == 0) {
     for (int i = 0; i < PR_XS; ++i) {
       asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(x_full + 8 * i), "r"(TMA ? 1 : 6) : "memory");
@@ -184,6 +190,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
       asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(d_full + 8 * i) : "memory");
       asm volatile("mbarrier.init.shared::cta.b64 [%0], 16;" ::"r"(d_empty + 8 * i) : "memory");
     }
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(all_done) : "memory");
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 20) {
@@ -305,10 +312,10 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
     const unsigned a_there = pr_there(a_full, first);
     PrRing<PR_CS> cr;
     PrRing<2> ar;
-    for (long long tile = tile0; tile < tiles; tile += tile_on) {
+    for (long long tile = tile0; tile < tiles && ok; tile += tile_on) {
 #pragma unroll 1
       for (int c = 0; c < n_chunks; ++c) {
-        if (ok && (c & 1) == 0) ok = code_wait(c_full + 8 * cr.at, cr.parity);
+        if ((c & 1) == 0) ok = code_wait(c_full + 8 * cr.at, cr.parity);
         unsigned w[4][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -316,6 +323,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
                        : "r"(my_codes + cr.at * PR_CODES + ((((unsigned)(c & 1) * 4u + (unsigned)j) ^ (unsigned)(r & 7)) << 4)) : "memory");
         if (ok) ok = code_wait(a_empty + 8 * ar.at, ar.parity ^ 1u);
         ok = __all_sync(0xffffffffu, ok);
+        if (!ok) break;   // (the buffer may be in use, the codes may not be there: no products of them)
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -392,6 +400,9 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
             ar.next();
           }
         }
+        // (products under way, of which none is when the block ends, also where a wait ran out)
+        if (chosen) pr_commit(all_done, (unsigned short)(1u << first));
+        code_wait(all_done, 0u);
       }
     } else if (!TMA || warp == 21 || warp == 22) {   // ---- the copies: with TMA X by one thread, the codes, which are further ahead, by another
       PrRing<PR_XS> xr;
@@ -405,8 +416,10 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
           if (warp == (TMA ? 22 : 21) && lane == 0 && (c & 1) == 0) {
             if (c_filled) ok = code_wait(c_empty + 8 * cr.at, cr.parity ^ 1u);
             if (ok) {
-              pr_expect(c_full + 8 * cr.at, PR_CODES);
-              pr_tma(codes0 + cr.at * PR_CODES, &map_codes, (chunk0 + c) * (PR_K / 2), (int)row0, c_full + 8 * cr.at);
+              if (c != p.missing) {
+                pr_expect(c_full + 8 * cr.at, PR_CODES);
+                pr_tma(codes0 + cr.at * PR_CODES, &map_codes, (chunk0 + c) * (PR_K / 2), (int)row0, c_full + 8 * cr.at);
+              }
               cr.next();
               if (cr.at == 0) c_filled = true;
             }
@@ -416,7 +429,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
             const unsigned at = x0_at + xr.at * Cfg::X_STAGE;
             if (TMA) {
               if (warp == 21 && lane == 0) {
-                if (x_filled && ok) ok = code_wait(x_empty + 8 * xr.at, xr.parity ^ 1u);
+                if (x_filled) ok = code_wait(x_empty + 8 * xr.at, xr.parity ^ 1u);
                 if (ok) {
                   if (rank == 0) pr_expect(x_full + 8 * xr.at, 2 * Cfg::X_STAGE);   // (of both blocks)
 #pragma unroll
@@ -426,7 +439,8 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
               }
             } else {
               if (x_filled && ok) ok = code_wait(x_empty + 8 * xr.at, xr.parity ^ 1u);
-              ok = __all_sync(0xffffffffu, ok);   // (warps stay together whatever comes of it)
+              ok = __all_sync(0xffffffffu, ok);
+              if (!ok) break;   // (the stage may be in use)
               // (what PR_ASK words need is asked for before the first is looked at)
               for (int i0 = tid - 21 * 32; i0 < HN * 8; i0 += 96 * PR_ASK) {
                 uint4 a[PR_ASK], b[PR_ASK];
@@ -455,16 +469,16 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
               __syncwarp();
               if (lane == 0) pr_arrive_first_written(x_there + 8 * xr.at);
             }
+            if (!ok) break;
             xr.next();
             if (xr.at == 0) x_filled = true;
           }
         }
       }
-      // nothing is left under way when the block ends: every stage that was filled has been waited for by those who read it, unless
-      // they gave up
-      if (lane == 0 && !ok) {
-        for (int i = 0; i < 2 * PR_CS; ++i) code_wait(c_full + 8 * (i % PR_CS), (unsigned)(i / PR_CS));
-        for (int i = 0; i < 2 * PR_XS; ++i) code_wait((rank == 0 ? x_full : x_empty) + 8 * (i % PR_XS), (unsigned)(i / PR_XS));
+      // nothing is left under way when the block ends, whoever gave up (what X the second block asked for the first one's barrier counts)
+      if (lane == 0) {
+        if (warp == (TMA ? 22 : 21)) cr.drain(c_full);
+        if (TMA && warp == 21 && rank == 0) xr.drain(x_full);
       }
     }
   }
