@@ -352,10 +352,11 @@ int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_t ldx, cons
  * element type t_type; 1 <= top <= IDKM_DISTILL_MAX_TOP):
  *   p_j = softmax_j(t_j / tau) over the entries with 0 <= idx_j < vocab (others do not count: pad with -1),
  *   q_v = softmax_v(z_v / tau),
- *   loss_out[row] = tau^2 sum_j p_j (ln p_j - ln q_{idx_j})                (terms with p_j = 0 are 0),
+ *   loss_out[row] = tau^2 sum_j p_j (ln p_j - ln q_{idx_j})       (terms with p_j below 2^-126 max p are 0),
  *   dz_out[row][v] = weight[row] tau (q_v - sum_{j: idx_j = v} p_j).
  * An index given twice counts twice.  A row without entries that count, or whose logits t are all -inf, has loss and gradient
- * 0.  Logits z of -inf (masked classes) have q = 0; where the teacher has p > 0 for one the loss is +inf.  A row z without a
+ * 0.  Logits z of -inf (masked classes) have q = 0; where the teacher has p > 0 for one the loss is +inf (p from 2^-126 max p on, as
+ * fp32 holds exp((t_j - max t) / tau): a class that the teacher masks with -1e4, say, counts for nothing).  A row z without a
  * finite logit has NaN.  weight (DEVICE, fp32 [rows], finite, NULL: 1) is dL/dloss of the row.  fp32 arithmetic; vocab <= 2^30, tau a
  * normal number.  Waits inside are bounded; results are NaN where one ran out.
  *   idkm_distill_forward   writes the loss (fp32 [rows]) and, for the backward, stats_out (fp32 [rows][2], or NULL): the

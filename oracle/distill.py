@@ -2,7 +2,9 @@
 row from the definition
 
   p_j = softmax_j(t_j / tau) over entries with 0 <= idx_j < V,   q = softmax(z / tau),
-  loss = tau^2 sum_j p_j (ln p_j - ln q_{idx_j}),   dz_v = w tau (q_v - sum_{j: idx_j = v} p_j).
+  loss = tau^2 sum_j p_j (ln p_j - ln q_{idx_j}),   dz_v = w tau (q_v - sum_{j: idx_j = v} p_j);
+
+p_j below 2^-126 of the largest, which fp32 holds as 0, has no term in the loss (on a class with q = 0 it would be infinite).
 """
 from __future__ import annotations
 
@@ -35,7 +37,7 @@ def distill(z, idx, t, tau: float, weight=None):
         for j, l in zip(at, lp):
             p = np.exp(l)
             ps[r, j] = p
-            if p > 0:
+            if l - lp.max() >= -126 * np.log(2.0):
                 loss[r] += tau * tau * p * (l - lq[idx[r, j]])
             dz[r, idx[r, j]] -= w * tau * p
     return loss, dz, ps, lqs

@@ -2,7 +2,7 @@
 // its gradient with respect to the student's logits.  For a row z in R^V, teacher entries (i_j, t_j), temperature tau:
 //   p_j = softmax_j(t_j / tau) over the entries with 0 <= i_j < V,   q_v = softmax_v(z_v / tau),
 //   loss = tau^2 sum_j p_j (ln p_j - ln q_{i_j}),    dz_v = w tau (q_v - sum_{j: i_j = v} p_j).
-// A row without entries (or whose t_j are all -inf) has loss 0 and gradient 0.  As sum_j p_j = 1,
+// A row without entries (or whose t_j are all -inf) has loss 0 and gradient 0; p_j below 2^-126 of the largest is 0 in the loss.  As sum_j p_j = 1,
 //   loss = tau^2 (sum_j p_j (t_j - z_{i_j}) / tau - L_t + L_z),   L_t, L_z the logarithms of the two normalisers.
 //
 // One pass over z.  A row is a cluster of as few blocks as hold it (8 vectors of 16 bytes a thread, up to 8 blocks); a thread sums
@@ -60,7 +60,8 @@ __device__ __forceinline__ float distill_ex2(float x) {
 // NaN has one in its sum.
 struct DistillPart {
   float m, s;        // student
-  float tm, ts, ta;  // teacher: largest t, sum of exp((t - tm) / tau), sum of that times t - z over the block's own entries
+  float tm, ts, ta;  // teacher: largest t, sum of exp((t - tm) / tau), sum of that times t - z over the block's own entries with z > -inf
+  float tx;          // ... largest t of those with z = -inf
 };
 
 // exp((m - top) / tau), 0 where m is -inf (an empty part, whatever top is).
@@ -85,12 +86,12 @@ __device__ __forceinline__ float distill_warp_sum(float x) {
 // Joins the warps' parts, lane i < WARPS holding that of warp i (other lanes an empty one): all lanes get the block's.
 template <int WARPS>
 __device__ __forceinline__ DistillPart distill_join(DistillPart a, float c2) {
-  const float inf = __int_as_float(0x7f800000);
   const float M = distill_warp_max(a.m), T = distill_warp_max(a.tm);
   const float g = distill_scale(a.tm, T, c2);
   a.s = distill_scaled(a.s, distill_scale(a.m, M, c2));
   a.ts = distill_scaled(a.ts, g);
-  a.ta = a.ta == inf ? inf : distill_scaled(a.ta, g);   // (mass of the teacher, however small, on a logit of -inf)
+  a.ta = g == 0.f ? 0.f : a.ta * g;   // (sums that overflowed next to the warp's largest t, too)
+  a.tx = distill_warp_max(a.tx);
 #pragma unroll
   for (int o = WARPS >> 1; o > 0; o >>= 1) {
     a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
@@ -102,6 +103,7 @@ __device__ __forceinline__ DistillPart distill_join(DistillPart a, float c2) {
   a.s = __shfl_sync(0xffffffffu, a.s, 0);
   a.ts = __shfl_sync(0xffffffffu, a.ts, 0);
   a.ta = __shfl_sync(0xffffffffu, a.ta, 0);
+  if (distill_scale(a.tx, T, c2) > 0.f) a.ta = __int_as_float(0x7f800000);   // (mass that is not 0 next to the row's largest)
   return a;
 }
 
@@ -405,16 +407,18 @@ __global__ void __launch_bounds__(BLOCK, 512 / BLOCK) idkm_distill_rows(const __
     a.s = distill_warp_sum(distill_scaled(sum, distill_scale(m, a.m, c2)));
     a.tm = none;
     a.ts = a.ta = 0.f;
+    a.tx = none;
     if (warp * 32 < p.top) {
       a.tm = distill_warp_max(t);
       const float u = t == none ? 0.f : distill_ex2((t - a.tm) * c2);
       a.ts = distill_warp_sum(u);
-      const float z = to_f32(own), term = z == none ? -none : u * (t - z);
-      a.ta = distill_warp_sum(mine && t != none ? term : 0.f);
+      const float z = to_f32(own);
+      a.ta = distill_warp_sum(mine && t != none && z != none ? u * (t - z) : 0.f);
+      a.tx = distill_warp_max(mine && z == none ? t : none);
     }
     if (lane == 0) s_warp[turn][warp] = a;
     __syncthreads();
-    const DistillPart empty = {none, 0.f, none, 0.f, 0.f};
+    const DistillPart empty = {none, 0.f, none, 0.f, 0.f, none};
     a = distill_join<WARPS>(lane < WARPS ? s_warp[turn][lane] : empty, c2);
     if (parts > 1 && warp == 0) {
       // (the next row's parts go to the other turn's places; those of the row after are sent once every block has sent the next
