@@ -261,7 +261,6 @@ __global__ void __launch_bounds__(GROUPS_BLOCK, 4) idkm_groups_short(const __gri
   const unsigned from = blockIdx.x * (GROUPS_BLOCK / 32) + (threadIdx.x >> 5), rows_on = n_warps / per_row, on = n_warps - rows_on * per_row;
   long long row = from / per_row;
   unsigned part = from - (unsigned)row * per_row;
-  bool ready = false;
   GroupsRaw<TW> raw[GROUPS_PIECES];
   auto fetch = [&](const TW* w, int c0) {
 #pragma unroll
@@ -284,14 +283,11 @@ __global__ void __launch_bounds__(GROUPS_BLOCK, 4) idkm_groups_short(const __gri
       }
     }
   };
-  while (row < p.rows) {
-    const TW* w_row = reinterpret_cast<const TW*>(p.W) + row * p.ldw;
+  for (bool first = true;; first = false) {
     const int c0 = (int)part * span + lane * GROUPS_LANE;
-    fetch(w_row, c0);
-    if (!ready) {   // (while the first weights are on their way)
-      groups_table<T>(t, p.C, p.k);
-      ready = true;
-    }
+    if (row < p.rows) fetch(reinterpret_cast<const TW*>(p.W) + row * p.ldw, c0);
+    if (first) groups_table<T>(t, p.C, p.k);   // (all warps of the block, those without work too, while the first weights are on their way)
+    if (row >= p.rows) break;
     unsigned char* to = p.codes + row * p.pitch;
     T* scales = reinterpret_cast<T*>(p.scales) + row * p.n_groups;
 #pragma unroll
@@ -328,8 +324,6 @@ __global__ void __launch_bounds__(GROUPS_BLOCK, 4) idkm_groups_short(const __gri
       ++row;
     }
   }
-  // (blocks have a warp with work each; a warp without waits for the table with the others)
-  if (!ready) groups_table<T>(t, p.C, p.k);
 }
 
 // Longer groups: a block each, which reads the group twice (the second time from L2).
