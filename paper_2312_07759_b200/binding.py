@@ -256,20 +256,39 @@ def _run(stream, call, first, *others):
 
 
 def _apart(out, *inputs) -> None:
-    """A given output may not share memory with an input."""
-    base, span = out.untyped_storage().data_ptr(), None
+    """A given output may not share memory with an input (rows of either may lie between the other's)."""
+    base, rows = out.untyped_storage().data_ptr(), None
     for t in inputs:
         if t is not None and t.untyped_storage().data_ptr() == base and t.numel():
-            if span is None:
-                span = _span(out)
-            a, b = _span(t)
-            if a < span[1] and span[0] < b:
+            if rows is None:
+                rows = _rows(out)
+            if _meet(rows, _rows(t)):
                 raise ValueError("the output shares memory with an input")
 
 
-def _span(t):
-    a = t.data_ptr()
-    return a, a + (sum((n - 1) * st for n, st in zip(t.shape, t.stride())) + 1) * t.element_size()
+def _rows(t):
+    """(first byte, rows, bytes from one to the next, bytes of one) of a tensor whose rows are contiguous."""
+    size, at = t.element_size(), t.data_ptr()
+    if t.is_contiguous():
+        return at, 1, 1, t.numel() * size
+    rows, cols, ld = _matrix(t)
+    return at, rows, max(ld * size, 1), cols * size
+
+
+def _meet(x, y) -> bool:
+    """Whether a byte of x's rows is one of y's."""
+    (a, n, p, u), (b, m, q, v) = x, y
+    if a + (n - 1) * p + u <= b or b + (m - 1) * q + v <= a:
+        return False
+    if n > m:
+        (a, n, p, u), (b, m, q, v) = y, x
+    if p == q:   # only the difference of two rows' numbers counts: one row of x, and as many of y as there are differences
+        b, m, n = b - (n - 1) * q, m + n - 1, 1
+    for i in range(n):   # rows j of y with b + j q < end of x's row and b + j q + v > its beginning
+        at = a + i * p
+        if max(0, (at - v - b) // q + 1) <= min(m - 1, (at + u - 1 - b) // q):
+            return True
+    return False
 
 
 def assign_groups(W, Cm, group: int, want_Wq: bool = False, stream=None):
@@ -311,8 +330,8 @@ def matmul_codes(X, codes, Cm, scales=None, group: int = 0, out=None, stream=Non
     if out is not None:
         if out.shape != (tokens, rows) or out.dtype != X.dtype or out.device != X.device:
             raise ValueError(f"an output of shape ({tokens}, {rows}) and of X's type and device expected")
-        _apart(out, X, codes, Cm, scales)
         ldy = _matrix(out)[2]
+        _apart(out, X, codes, Cm, scales)
 
     def call(handle):
         Y = X.new_empty((tokens, rows)) if out is None else out
@@ -357,8 +376,8 @@ def _distill_out(z, out, *inputs):
         return z.shape[1]
     if out.shape != z.shape or out.dtype != z.dtype or out.device != z.device:
         raise ValueError("an output of z's shape, type and device expected")
-    _apart(out, *inputs)
     ld = _matrix(out)[2]
+    _apart(out, *inputs)
     if out.data_ptr() != z.data_ptr() or ld != _matrix(z)[2]:
         _apart(out, z)
     return ld
