@@ -3,6 +3,10 @@
 Argument marshalling only: every step of the path runs in the library's CUDA kernels.  PyTorch
 supplies device memory (``tensor.data_ptr()``) and the current stream.  Importing this module
 raises if the library has not been built; there is no CPU fallback.
+
+Calls take a ``stream``.  Those on codes with group scales and on logits (``assign_groups``, ``matmul_codes``,
+``distill_*``) mark their tensors as used on it; for the others, and for a ``Context``'s, the caller keeps the
+tensors of a call until that stream is past it.
 """
 from __future__ import annotations
 
@@ -215,11 +219,12 @@ def _matrix(t):
 
 class _Place:
     """Where a call runs that does not run on the current stream of the current device: inside the ``with`` that device is
-    current, and new tensors belong to that stream."""
-    __slots__ = ("handle", "_with")
+    current, and new tensors belong to that stream.  ``given``: the stream, if one was given."""
+    __slots__ = ("handle", "given", "_with")
 
     def __init__(self, stream, dev):
         import torch
+        self.given = None
         if stream is None:
             self._with = torch.cuda.device(dev)
             self.handle = torch.cuda.current_stream(dev).cuda_stream or None
@@ -228,6 +233,7 @@ class _Place:
             stream = torch.cuda.ExternalStream(int(stream), device=dev)
         if stream.device.index != dev:
             raise ValueError(f"a stream of device {dev} expected, not of {stream.device}")
+        self.given = stream
         self._with = torch.cuda.stream(stream)
         self.handle = int(stream.cuda_stream) or None
 
@@ -241,7 +247,8 @@ class _Place:
 
 def _run(stream, call, first, *others):
     """``call(stream handle)`` on the device of the tensors, which have to be on one, and on ``stream``, or that device's current
-    one.  (A call on the current device's current stream, the usual case, costs no context manager.)"""
+    one.  (A call on the current device's current stream, the usual case, costs no context manager.)  The memory of the tensors
+    is not handed out again before a given stream is past the call, even if the caller lets go of them right after it."""
     import torch
     dev = first.get_device()
     if dev < 0:
@@ -252,7 +259,12 @@ def _run(stream, call, first, *others):
     if stream is None and torch._C._cuda_getDevice() == dev:
         return call(torch._C._cuda_getCurrentRawStream(dev) or None)
     with _Place(stream, dev) as at:
-        return call(at.handle)
+        made = call(at.handle)
+    if at.given is not None:
+        for t in (first, *others):
+            if t is not None:
+                t.record_stream(at.given)
+    return made
 
 
 def _apart(out, *inputs) -> None:
@@ -338,7 +350,7 @@ def matmul_codes(X, codes, Cm, scales=None, group: int = 0, out=None, stream=Non
         return Y, lib.idkm_matmul_codes(X.data_ptr(), e, tokens, ldx, codes.data_ptr(), rows, cols, pitch, Cm.data_ptr(), Cm.numel(),
                                         None if scales is None else scales.data_ptr(), group, Y.data_ptr(), ldy, handle)
 
-    Y, rc = _run(stream, call, X, codes, Cm, scales)
+    Y, rc = _run(stream, call, X, codes, Cm, scales, out)
     if rc:
         raise IdkmError(rc)
     return Y
