@@ -333,10 +333,11 @@ int64_t idkm_group_codes_pitch(int64_t cols);   /* 16 ceil(cols / 32); 0 for col
  * all DEVICE; codes as idkm_assign_groups writes them, rows `pitch` bytes apart (a multiple of 16, at least 16 ceil(cols / 32);
  * the bytes of a row up to there are read, codes past the last column count for nothing).  scales = NULL: all 1 (the codes of
  * idkm_assign for a layer of 5 <= k <= 16 scalar centroids and rows of a multiple of 32 weights).  Products and sums are in
- * fp32, the scale multiplies the fp32 sum of its group, and Y is rounded once; the order of the sums depends on the shape
- * and the GPU alone.  C must be finite; a code that names no entry stands for 0.  codes 16-byte aligned, the others to their elements
+ * fp32; the scale multiplies fp32 sums of up to 128 columns of its group (of eight columns where `type` is fp32), and Y is rounded
+ * once; the order of the sums depends on the shape and the GPU alone.  C must be finite; a code that names no entry stands for 0.  codes 16-byte aligned, the others to their elements
  * (X is read fastest from 16-byte-aligned rows).  group as above, or any number >= cols: one scale a row.  Tokens, rows and columns
- * up to 2^31 - 4097 each.  Y may not overlap an input.  Waits inside are bounded; Y is NaN where one ran out.  No context, no
+ * up to 2^31 - 4097 each.  Y may not overlap an input (its rows may lie between an input's).  Waits inside are bounded, by about a
+ * second each; Y is NaN where one ran out.  No context, no
  * workspace; asynchronous on cuda_stream.  Returns as idkm_assign_groups.
  */
 int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_t ldx, const unsigned char* codes, int64_t rows, int64_t cols,
@@ -361,7 +362,10 @@ int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_t ldx, cons
  * normal number.  Waits inside are bounded; results are NaN where one ran out.
  *   idkm_distill_forward   writes the loss (fp32 [rows]) and, for the backward, stats_out (fp32 [rows][2], or NULL): the
  *                          logarithms of the student's and of the teacher's normaliser, in units of logits / tau;
- *   idkm_distill_backward  writes dz (rows lddz elements apart, type of z) from the same inputs and those statistics;
+ *   idkm_distill_backward  writes dz (rows lddz elements apart, type of z) from the same inputs and those statistics, which as
+ *                          fp32 hold a logarithm L to 2^-24 |L|: q is off by that much of its value, so it says nothing where
+ *                          |z| / tau is as large as 2^24 for all of a row (one whose classes are all masked by the type's
+ *                          lowest value, say; idkm_distill_step keeps z - max z there);
  *   idkm_distill_step      both in one launch, z read once where a row fits on the chip.
  * dz_out may be z itself (with lddz = ldz), otherwise it may not overlap an input.  No context, no workspace; asynchronous on
  * cuda_stream.  Returns IDKM_OK, IDKM_ERR_NULL, IDKM_ERR_UNSUPPORTED (types, top), IDKM_ERR_SHAPE, IDKM_ERR_PARAM (tau),
