@@ -457,9 +457,9 @@ int idkm_set_collapse_step(idkm_ctx* ctx, int method);
 int idkm_set_test_hooks(idkm_ctx* ctx, int missing_arrivals, int64_t spin_limit_ticks);
 
 /*
- * The same for idkm_matmul_codes with many rows of 16-bit X (its kernel for prompts), which has no ctx: for the calls of this process
- * that follow.  missing_copy = n > 0: every block's n-th copy of codes of a tile (256 columns of its share) is never asked for, so the
- * waits for it run out, after about a second each.  0 restores production behaviour, which is also the state at the start.  Returns
+ * The same for idkm_matmul_codes with 16-bit X, which has no ctx: for the calls of this process that follow.  missing_copy = n > 0:
+ * every block's n-th copy of codes of a tile (256 columns of its share; with few rows of X every copy) never arrives, so the waits
+ * for it run out, after about a second each, and results are NaN.  0 restores production behaviour, which is also the state at the start.  Returns
  * IDKM_OK or IDKM_ERR_PARAM (a negative argument, or one above 2^24).
  */
 int idkm_set_codes_test_hooks(int missing_copy);

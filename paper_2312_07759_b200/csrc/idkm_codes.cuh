@@ -18,7 +18,7 @@ struct CodesParams {
   void* Y;
   long long ldy;
   int vec_x;   // rows of X start on 16-byte boundaries
-  int missing;   // of many rows of X: the chunk from which codes are not copied (a test's; below 0: none)
+  int missing;   // 16-bit X: the copy of codes that is left out (a test's; below 0: none)
 };
 
 // Products for many rows of 16-bit X, on the tensor cores (idkm_codes_prompt.cu).

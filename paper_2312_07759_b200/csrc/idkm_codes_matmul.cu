@@ -212,6 +212,7 @@ struct FewPlan {
   unsigned per_group;   // strip * per_group >> 20 is the group of a strip (strips below 2^10, a group's below 2^9; for longer ones 0)
   __host__ __device__ int scale_bytes() const { return 2 * tiles * FEW_ROWS * scale_words * 4; }   // of two batches
   int kept;                      // bytes of the sums that are kept
+  int awaited;                   // bytes that every copy is waited for beyond its own: 0 (16 in a test of waits that run out)
 };
 
 // The i-th 16 of the sums that meet, in the free halves of the table's rows.
@@ -245,24 +246,24 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
     asm volatile("bar.arrive 2, %0;" ::"n"(FEW_BLOCK + 32) : "memory");   // (the barriers are ready)
     if (lane < FEW_ROWS) {
       int stage = 0, turn = 0;
-      bool filled = false;   // every stage has been filled once
-      for (int round = tile0; round < tile1; round += f.round) {
+      bool filled = false, ok = true;   // every stage has been filled once; no wait has run out
+      for (int round = tile0; round < tile1 && ok; round += f.round) {
         const int end = PARTS ? min(round + f.round, tile1) : tile1;
-        for (int chunk0 = 0; chunk0 < all_chunks; chunk0 += slab) {
+        for (int chunk0 = 0; chunk0 < all_chunks && ok; chunk0 += slab) {
           const int chunks = PARTS ? min(slab, all_chunks - chunk0) : all_chunks;
-          for (int batch = round; batch < end; batch += f.tiles) {
+          for (int batch = round; batch < end && ok; batch += f.tiles) {
             const int steps = min(f.tiles, end - batch) * chunks;
             int tile = batch, chunk = 0;
             for (int s = 0; s < steps; s += FEW_WARPS) {
               const unsigned bar = full + 8 * stage;
-              if (filled && !code_wait(empty + 8 * stage, (turn & 1) ^ 1)) return;
+              if (filled && !(ok = code_wait(empty + 8 * stage, (turn & 1) ^ 1))) break;
               unsigned to = stage0 + stage * FEW_STAGE + lane * FEW_PITCH;
               for (int left = min(FEW_WARPS, steps - s); left > 0;) {
                 const int n = min(left, chunks - chunk);
                 const long long row = (long long)tile * FEW_ROWS + lane;
                 const int at = (chunk0 + chunk) * (FEW_CHUNK / 2), bytes = min(n * (FEW_CHUNK / 2), code_bytes - at);
                 if (row < p.rows) {   // (what is not copied is what was there: codes of rows or columns past the last count for nothing)
-                  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+                  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes + f.awaited) : "memory");
                   asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                                ::"r"(to), "l"(p.codes + row * p.pitch + at), "r"(bytes), "r"(bar) : "memory");
                 }
@@ -286,6 +287,8 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
         }
         if (!PARTS) break;
       }
+      // (no copy is under way when the block ends, also where the others gave up waiting for one)
+      for (int i = 0; i < f.stages; ++i) code_wait(full + 8 * i, i < stage ? turn : turn ^ 1);
     }
     return;
   }
@@ -357,7 +360,7 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
   }
   const unsigned my_codes = stage0 + gid * FEW_PITCH + warp * (FEW_CHUNK / 2) + tig * 16;
   int stage = 0, stage_turn = 0, turn = 0;
-  bool lost = false;   // a wait ran out (none does: the copies wait for nothing but these warps); later ones do not wait
+  bool lost = false;   // a wait ran out (none does: the copies wait for nothing but these warps); later ones do not wait, nothing is handed back
   float tot[NT][4];
 #pragma unroll
   for (int n = 0; n < NT; ++n)
@@ -500,7 +503,7 @@ __global__ void __launch_bounds__(FEW_BLOCK + 32, 1) idkm_codes_few(const __grid
           }
           // (the codes have been used, so they have been read)
           __syncwarp();
-          if (lane == 0) code_arrive(empty + 8 * stage);
+          if (lane == 0 && !lost) code_arrive(empty + 8 * stage);   // (a stage whose codes may be still to come is not filled again)
           if (++stage == f.stages) {
             stage = 0;
             stage_turn ^= 1;
@@ -577,6 +580,7 @@ template <class T, int Q, bool SCALED>
 cudaError_t few_launch(const CodesParams& p, int sms, cudaStream_t st) {
   const int tiles = (int)((p.rows + FEW_ROWS - 1) / FEW_ROWS), blocks = tiles < sms ? tiles : sms;
   FewPlan f = few_plan(p, (tiles + blocks - 1) / blocks);
+  f.awaited = p.missing < 0 ? 0 : 16;
   f.per_block = tiles / blocks;
   f.extra = tiles % blocks;
   const bool parts = f.kept > 0;
@@ -663,7 +667,7 @@ extern "C" int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_
   p.n_groups = (cols + p.group - 1) / p.group;
   p.Y = Y; p.ldy = ldy;
   p.vec_x = (uintptr_t)X % 16 == 0 && ldx * tb % 16 == 0;
-  p.missing = 2 * hook_missing_copy.load(std::memory_order_relaxed) - 2;
+  p.missing = hook_missing_copy.load(std::memory_order_relaxed) - 1;
   cudaStream_t st = reinterpret_cast<cudaStream_t>(cuda_stream);
   if (type == ELEM_F32) return rows_launch(p, sms, st) == cudaSuccess ? IDKM_OK : IDKM_ERR_CUDA;
   const bool few = tokens <= FEW_TOKENS;

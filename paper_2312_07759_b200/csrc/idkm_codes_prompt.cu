@@ -416,7 +416,7 @@ __global__ void __launch_bounds__(PR_BLOCK, 1) idkm_codes_prompt(const __grid_co
           if (warp == (TMA ? 22 : 21) && lane == 0 && (c & 1) == 0) {
             if (c_filled) ok = code_wait(c_empty + 8 * cr.at, cr.parity ^ 1u);
             if (ok) {
-              if (c != p.missing) {
+              if (c / 2 != p.missing) {
                 pr_expect(c_full + 8 * cr.at, PR_CODES);
                 pr_tma(codes0 + cr.at * PR_CODES, &map_codes, (chunk0 + c) * (PR_K / 2), (int)row0, c_full + 8 * cr.at);
               }
