@@ -359,7 +359,7 @@ int idkm_matmul_codes(const void* X, int type, int64_t tokens, int64_t ldx, cons
  * 0.  Logits z of -inf (masked classes) have q = 0; where the teacher has p > 0 for one the loss is +inf (p from 2^-126 max p on, as
  * fp32 holds exp((t_j - max t) / tau): a class that the teacher masks with -1e4, say, counts for nothing).  A row z without a
  * finite logit has NaN.  weight (DEVICE, fp32 [rows], finite, NULL: 1) is dL/dloss of the row.  fp32 arithmetic; vocab <= 2^30, tau a
- * normal number.  Waits inside are bounded; results are NaN where one ran out.
+ * normal number.  Waits inside are bounded, by about a second each; results are NaN where one ran out.
  *   idkm_distill_forward   writes the loss (fp32 [rows]) and, for the backward, stats_out (fp32 [rows][2], or NULL): the
  *                          logarithms of the student's and of the teacher's normaliser, in units of logits / tau;
  *   idkm_distill_backward  writes dz (rows lddz elements apart, type of z) from the same inputs and those statistics, which as

@@ -28,7 +28,7 @@ namespace {
 using namespace idkm;
 
 constexpr int DISTILL_MAX_CLUSTER = 8;
-constexpr int DISTILL_POLLS = 1 << 22;   // (each waits for some time itself)
+constexpr int DISTILL_POLLS = 1 << 19;   // (each waits for some time itself, 2 us: about a second)
 constexpr float LOG2E = 1.4426950408889634f, LOG2E_LOW = (float)(1.4426950408889634 - (double)1.4426950408889634f);
 
 struct DistillParams {
@@ -331,7 +331,7 @@ __global__ void __launch_bounds__(BLOCK, 512 / BLOCK) idkm_distill_rows(const __
   }
   const uint32_t bar = (uint32_t)__cvta_generic_to_shared(s_bar);
   uint32_t there = 0, there_bar = 0, phase = 0;
-  bool lost = false;   // a wait ran out (it does not: a cluster's blocks run together); later ones do not wait
+  bool lost = false;   // a wait ran out (it does not: a cluster's blocks run together); later ones do not wait, nothing more is sent
   if (parts > 1) {
     if (tid == 0) {
       asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar) : "memory");
@@ -420,7 +420,7 @@ __global__ void __launch_bounds__(BLOCK, 512 / BLOCK) idkm_distill_rows(const __
     __syncthreads();
     const DistillPart empty = {none, 0.f, none, 0.f, 0.f, none};
     a = distill_join<WARPS>(lane < WARPS ? s_warp[turn][lane] : empty, c2);
-    if (parts > 1 && warp == 0) {
+    if (parts > 1 && warp == 0 && !lost) {
       // (the next row's parts go to the other turn's places; those of the row after are sent once every block has sent the next
       // row's, and so has read these.  Sent with their arrival: a cluster barrier would wait for this thread's stores to dz too)
       if (tid == 0) asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar + 8 * turn), "r"(16 * parts) : "memory");
@@ -474,6 +474,7 @@ __global__ void __launch_bounds__(BLOCK, 512 / BLOCK) idkm_distill_rows(const __
       }
       a.m = M;
       if (lost) a.s = __int_as_float(0x7fc00000);
+      if (next >= p.rows) asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory");
     }
     if (MODE == DISTILL_STEP) {
       const float wt = p.tau * w, scale = __fdividef(wt, a.s), f = LONG ? scale : distill_scale(m, a.m, c2) * scale;
@@ -530,6 +531,8 @@ __global__ void __launch_bounds__(BLOCK, 512 / BLOCK) idkm_distill_rows(const __
     }
     at = at1; t = t1; own = own1; w = w1;
   }
+  // (no block leaves while another, whose wait for it may have run out, can still send it something)
+  if (parts > 1) asm volatile("barrier.cluster.wait;" ::: "memory");
 }
 
 // The gradient alone, from the normalisers that the loss left: a block takes NV vectors a thread of one row.
